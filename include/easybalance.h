@@ -35,10 +35,14 @@
  *    that easybalance_moe_step reads (see easybalance_pack_weights).
  *    "dtype" is the model's storage type (EB_DTYPE_F32 or EB_DTYPE_BF16,
  *    bf16 as raw 16-bit patterns); accumulation is always fp32.
+ *    EB_DTYPE_FP8 stacks hold their experts in 8 bits with block scales (see
+ *    easybalance_pack_weights_fp8) and everything else (activations, outputs,
+ *    router weights: every "dtype" buffer below) in bf16.
  *  - Shape limits (EB_ERR_UNSUPPORTED otherwise): H % 256 == 0,
  *    F % 128 == 0, 1 <= k <= E, E + S <= 1024, k + S <= 16, E % D == 0,
- *    L <= EB_MAX_LAYERS, L * (E + S) <= 15360; bf16 stacks: E <= 256 and
- *    2F * H * 2 bytes < 2 GiB (one gate/up matrix).
+ *    L <= EB_MAX_LAYERS, L * (E + S) <= 15360; bf16 and 8-bit stacks: E <= 256
+ *    and one gate/up matrix (2F * H values) < 2 GiB; 8-bit steps: tokens * H and
+ *    4 * ceil(F / 512) * tokens * (k + S) below 2^31.
  */
 #ifndef EASYBALANCE_H
 #define EASYBALANCE_H
@@ -58,10 +62,14 @@ extern "C" {
 
 #define EB_DTYPE_F32 0
 #define EB_DTYPE_BF16 1
+#define EB_DTYPE_FP8 2          /* experts in e4m3 with block scales, the rest bf16 */
 
 #define EB_POLICY_MAXUTIL 0
 #define EB_POLICY_CUMUTIL 1
 #define EB_POLICY_DIFFPEAK 2
+#define EB_SCORE_SOFTMAX 0       /* eb_router scores */
+#define EB_SCORE_SIGMOID 1
+
 #define EB_WEIGHTS_GATE_UP 0     /* easybalance_pack_weights kinds */
 #define EB_WEIGHTS_DOWN 1
 
@@ -78,8 +86,10 @@ extern "C" {
 /* Kernel classes reported by the profiling calls.  A call reports the classes
  * of the kernels it launches: a router that also picks (fused or matrix-core)
  * is ROUTE_LOGITS, and ROUTE_TOPK its separate top-k and count launches, none
- * where the router counts too; the grouping of a small step runs as one
- * kernel, reported as PERM_SCAN (with the gather's copies in the smallest). */
+ * where the router counts too (the choice under an eb_router is always
+ * ROUTE_TOPK); the grouping of a small step runs as one
+ * kernel, reported as PERM_SCAN (with the gather's copies in the smallest); an
+ * 8-bit step gathers no rows, PERM_GATHER is the quantisation of its tokens. */
 #define EB_K_ROUTE_NORM 0
 #define EB_K_ROUTE_LOGITS 1
 #define EB_K_ROUTE_TOPK 2
@@ -167,6 +177,62 @@ int easybalance_route(const eb_model_desc* desc, int32_t layer, int32_t T, const
                       const float* gain, const void* Wg, const float* bias, void* a_out,
                       float* logits_out, int32_t* idx_out, float* w_out, int32_t* counts_out,
                       void* stream);
+
+/*
+ * How experts are chosen from router logits z, in place of the plain softmax
+ * top-k of easybalance_route:
+ *
+ *   s   = 1 / (1 + e^-z)  (EB_SCORE_SIGMOID)  or  softmax(z) over all E
+ *   c   = s + balance                 (balance: a per-expert bias that only the
+ *                                     choice sees, NULL = none)
+ *   of the n_group groups of E / n_group consecutive experts, the topk_group
+ *   with the largest group score stay; a group's score is the sum of its
+ *   group_top largest c (topk_group == n_group: all stay)
+ *   idx = the k largest c in the groups that stay, largest first
+ *   w   = scale * s[idx]  (norm_topk = 1: scale * s[idx] / sum_r s[idx_r];
+ *                          0 where that sum is 0)
+ *
+ * Larger first, equal ones by the lower id (expert or group); decided as if s
+ * and c were exact: values closer than fp32 resolves are compared in fp64.
+ * Logits and balance may be -inf (an expert that is only picked when nothing
+ * else is left); c = NaN ranks after every number, so the k picks are always
+ * distinct experts.  In a softmax row a NaN or +inf logit makes every s NaN, and
+ * a row of -inf alone has s = 0.
+ * Limits: n_group divides E, n_group <= 64, group_top 1 or 2 and at most the
+ * group's size where groups are left out, k <= topk_group * E / n_group, scale
+ * finite; E <= 1024, k <= 16.  norm_topk replaces the descriptor's.
+ */
+typedef struct eb_router {
+  int32_t score;        /* EB_SCORE_*                                       */
+  int32_t n_group, topk_group, group_top;
+  int32_t norm_topk;
+  float scale;
+} eb_router;
+
+/*
+ * easybalance_select -- experts, weights and counts of T tokens from their
+ * router logits, under `router` (see eb_router).  One launch for up to 32
+ * tokens, else two.
+ *
+ * logits     device [T][E] fp32
+ * balance    device [E] fp32, or NULL
+ * idx_out    device [T][k] int32
+ * w_out      device [T][k] fp32
+ * counts_out device [E] int32 (overwritten; zeros for T = 0)
+ */
+int easybalance_select(int32_t T, int32_t E, int32_t k, const eb_router* router, const float* logits,
+                       const float* balance, int32_t* idx_out, float* w_out, int32_t* counts_out, void* stream);
+
+/*
+ * easybalance_route_scored -- easybalance_route with the experts chosen under
+ * `router`: the same a and logits bit for bit, then the picks of
+ * easybalance_select.  Arguments as there; balance device [E] fp32 (this
+ * layer's) or NULL; logits_out is required (the choice reads it).
+ */
+int easybalance_route_scored(const eb_model_desc* desc, const eb_router* router, int32_t layer, int32_t T,
+                             const float* x, const float* gain, const void* Wg, const float* bias,
+                             const float* balance, void* a_out, float* logits_out, int32_t* idx_out,
+                             float* w_out, int32_t* counts_out, void* stream);
 
 /*
  * Static placement of every layer's experts on the D (virtual) devices, with
@@ -322,6 +388,49 @@ int easybalance_pack_weights(const eb_model_desc* desc, int32_t kind, int32_t n,
                              void* dst, void* stream);
 
 /*
+ * 8-bit experts (EB_DTYPE_FP8).  A weight matrix [N][K] is e4m3 values q (OCP:
+ * largest number 448, no infinities) with one fp32 scale for each 128 x 128
+ * block, scales [N/128][K/128]: w[n][k] = q[n][k] * scales[n/128][k/128].
+ * Scales are positive and normal (0 and subnormal ones count as 2^-127).
+ * easybalance_moe_step then quantises its activations the same way, by row and
+ * 128 columns: s the smallest power of two with max |v| <= 448 s (1 for zeros),
+ * q = e4m3(v / s) to nearest even, infinities and NaN as NaN (and left out of
+ * the maximum):
+ *   y = sum over blocks of s_a * scale * sum q_a q_w     (fp32 accumulate)
+ *   h = quantised( SiLU(y_gate) * y_up ),  o = bf16( h W_down^T )
+ * Its views: perm and offsets; a_perm and h must be NULL (EB_ERR_UNSUPPORTED),
+ * and easybalance_moe_step_noalloc does not take these stacks
+ * (easybalance_moe_step allocates nothing either).
+ *
+ * easybalance_quantize_weights -- n matrices in bf16 or fp32 to q and scales,
+ * by the rule above for each 128 x 128 block (so every scale is a power of two).
+ *
+ * desc      dtype EB_DTYPE_FP8; gives the matrix sizes
+ * kind, n   as for easybalance_pack_weights
+ * src_dtype EB_DTYPE_BF16 or EB_DTYPE_F32
+ * src       device [n][N][K] of src_dtype, row-major, 16-byte aligned
+ * q         device [n][N][K] e4m3, row-major, 8-byte aligned, written
+ * scales    device [n][N/128][K/128] fp32, written
+ * src, q and scales must not overlap.
+ */
+int easybalance_quantize_weights(const eb_model_desc* desc, int32_t kind, int32_t n, int32_t src_dtype,
+                                 const void* src, void* q, float* scales, void* stream);
+
+/*
+ * easybalance_pack_weights_fp8 -- 8-bit expert weights into the layout the
+ * grouped GEMMs stream: one buffer of easybalance_packed_fp8_size bytes a layer
+ * and kind (n = E + S), the matrices' blocks as in easybalance_pack_weights with
+ * 128 K columns (128 bytes) to a block row, then the n matrices' scales.
+ *
+ * q, scales device, row-major as above (the checkpoint's, or from
+ *           easybalance_quantize_weights); unchanged
+ * dst       device, 16-byte aligned, written; must overlap neither
+ */
+int easybalance_packed_fp8_size(const eb_model_desc* desc, int32_t kind, int32_t n, size_t* bytes);
+int easybalance_pack_weights_fp8(const eb_model_desc* desc, int32_t kind, int32_t n, const void* q,
+                                 const float* scales, void* dst, void* stream);
+
+/*
  * easybalance_combine -- the weighted sum of Eq. (1) plus the residual of
  * Section 2.1, for every micro-batch of the step (the gather half of
  * MoECompute_Combine):
@@ -398,6 +507,19 @@ int easybalance_run_pass(const eb_model_desc* desc, int32_t N, int32_t T, float*
                          int32_t* n_steps_out, uint64_t* runsets_out, int32_t* layers_out,
                          int64_t* step_load_out, int32_t* groups_out, int32_t* layer_loads_out,
                          const eb_placement* placement, void* stream);
+
+/*
+ * easybalance_run_pass_scored -- easybalance_run_pass with every routing done
+ * under `router` (host- and device-scheduled alike).  balance: device [L][E]
+ * fp32, or NULL; the rest as there.
+ */
+int easybalance_run_pass_scored(const eb_model_desc* desc, const eb_router* router, int32_t N, int32_t T, float* x,
+                                const float* gain, const void* const* Wg, const float* bias, const float* balance,
+                                const void* const* W_gu, const void* const* W_dn, int32_t policy, int32_t m,
+                                void* state, size_t state_bytes, int32_t max_steps, int32_t* n_steps_out,
+                                uint64_t* runsets_out, int32_t* layers_out, int64_t* step_load_out,
+                                int32_t* groups_out, int32_t* layer_loads_out, const eb_placement* placement,
+                                void* stream);
 
 /*
  * Kernel timing for measurement.  Between easybalance_profile_begin(mask) and

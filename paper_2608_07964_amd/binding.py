@@ -21,7 +21,8 @@ EB_ERR_INVALID_ARG = -1
 EB_ERR_UNSUPPORTED = -2
 EB_ERR_HIP = -3
 EB_ERR_WORKSPACE_TOO_SMALL = -4
-EB_DTYPE_F32, EB_DTYPE_BF16 = 0, 1
+EB_DTYPE_F32, EB_DTYPE_BF16, EB_DTYPE_FP8 = 0, 1, 2
+EB_SCORE_SOFTMAX, EB_SCORE_SIGMOID = 0, 1
 EB_POLICY_MAXUTIL, EB_POLICY_CUMUTIL, EB_POLICY_DIFFPEAK, EB_POLICY_LOCKSTEP = 0, 1, 2, 3
 EB_PASS_DEVICE_SCHEDULE = 0x100  # OR-ed into easybalance_run_pass's policy
 EB_WEIGHTS_GATE_UP, EB_WEIGHTS_DOWN = 0, 1
@@ -36,7 +37,9 @@ EXPORTS = ["easybalance_version", "easybalance_last_error", "easybalance_route",
            "easybalance_schedule", "easybalance_moe_step_workspace_size", "easybalance_moe_step",
            "easybalance_combine", "easybalance_profile_begin", "easybalance_profile_end",
            "easybalance_pass_state_size", "easybalance_run_pass", "easybalance_pack_weights",
-           "easybalance_moe_step_noalloc"]
+           "easybalance_moe_step_noalloc", "easybalance_select", "easybalance_route_scored",
+           "easybalance_run_pass_scored", "easybalance_quantize_weights", "easybalance_packed_fp8_size",
+           "easybalance_pack_weights_fp8"]
 EB_NOALLOC_SCRATCH_BYTES = 160 * 1024 * 1024
 
 
@@ -61,6 +64,17 @@ class eb_step_views(ctypes.Structure):
 class eb_placement(ctypes.Structure):
     _fields_ = [("L", ctypes.c_int32), ("E", ctypes.c_int32), ("D", ctypes.c_int32),
                 ("R", ctypes.c_int32), ("copies", ctypes.c_void_p)]
+
+
+class eb_router(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("n_group", ctypes.c_int32), ("topk_group", ctypes.c_int32),
+                ("group_top", ctypes.c_int32), ("norm_topk", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+def make_router(score="softmax", *, n_group=1, topk_group=1, group_top=2, norm_topk=1, scale=1.0) -> eb_router:
+    """score: "softmax", "sigmoid" or an EB_SCORE_* value."""
+    sc = score if isinstance(score, int) else {"softmax": EB_SCORE_SOFTMAX, "sigmoid": EB_SCORE_SIGMOID}[score]
+    return eb_router(sc, n_group, topk_group, group_top, norm_topk, scale)
 
 
 def make_placement(copies, D: int):
@@ -128,6 +142,20 @@ def lib() -> ctypes.CDLL:
                                        ctypes.POINTER(ctypes.c_int32), I64P,
                                        ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32),
                                        ctypes.POINTER(eb_placement), P]
+    R = ctypes.POINTER(eb_router)
+    l.easybalance_select.restype = ctypes.c_int
+    l.easybalance_select.argtypes = [I32, I32, I32, R, P, P, P, P, P, P]
+    l.easybalance_route_scored.restype = ctypes.c_int
+    l.easybalance_route_scored.argtypes = [D, R, I32, I32, P, P, P, P, P, P, P, P, P, P, P]
+    rp = list(l.easybalance_run_pass.argtypes)
+    l.easybalance_run_pass_scored.restype = ctypes.c_int
+    l.easybalance_run_pass_scored.argtypes = [rp[0], R, *rp[1:7], P, *rp[7:]]
+    l.easybalance_quantize_weights.restype = ctypes.c_int
+    l.easybalance_quantize_weights.argtypes = [D, I32, I32, I32, P, P, P, P]
+    l.easybalance_packed_fp8_size.restype = ctypes.c_int
+    l.easybalance_packed_fp8_size.argtypes = [D, I32, I32, SZP]
+    l.easybalance_pack_weights_fp8.restype = ctypes.c_int
+    l.easybalance_pack_weights_fp8.argtypes = [D, I32, I32, P, P, P, P]
     l.easybalance_pack_weights.restype = ctypes.c_int
     l.easybalance_pack_weights.argtypes = [D, I32, I32, P, P, P]
     l.easybalance_profile_begin.restype = ctypes.c_int
@@ -152,7 +180,7 @@ def _check(fn: str, rc: int) -> None:
 
 
 def make_desc(L, H, F, E, k, S, D, dtype, rms_eps=1e-6, norm_topk=0) -> eb_model_desc:
-    dt = dtype if isinstance(dtype, int) else (EB_DTYPE_BF16 if dtype == "bf16" else EB_DTYPE_F32)
+    dt = dtype if isinstance(dtype, int) else {"bf16": EB_DTYPE_BF16, "fp8": EB_DTYPE_FP8}.get(dtype, EB_DTYPE_F32)
     return eb_model_desc(L, H, F, E, k, S, D, dt, rms_eps, norm_topk)
 
 
@@ -169,6 +197,21 @@ def easybalance_route(desc, layer, T, x, gain, Wg, bias, a_out, logits_out, idx_
     _check("easybalance_route", lib().easybalance_route(
         ctypes.byref(desc), layer, T, _ptr(x), _ptr(gain), _ptr(Wg), _ptr(bias), _ptr(a_out),
         _ptr(logits_out), _ptr(idx_out), _ptr(w_out), _ptr(counts_out), stream))
+
+
+def easybalance_route_scored(desc, router, layer, T, x, gain, Wg, bias, balance, a_out, logits_out, idx_out, w_out,
+                             counts_out, stream=None) -> None:
+    """router: from make_router; balance: [E] fp32 or None."""
+    _check("easybalance_route_scored", lib().easybalance_route_scored(
+        ctypes.byref(desc), ctypes.byref(router), layer, T, _ptr(x), _ptr(gain), _ptr(Wg), _ptr(bias), _ptr(balance),
+        _ptr(a_out), _ptr(logits_out), _ptr(idx_out), _ptr(w_out), _ptr(counts_out), stream))
+
+
+def easybalance_select(T, E, k, router, logits, balance, idx_out, w_out, counts_out, stream=None) -> None:
+    """router: from make_router; balance: [E] fp32 or None."""
+    _check("easybalance_select", lib().easybalance_select(
+        T, E, k, ctypes.byref(router) if router is not None else None, _ptr(logits), _ptr(balance), _ptr(idx_out),
+        _ptr(w_out), _ptr(counts_out), stream))
 
 
 def easybalance_schedule(pool_ids, counts, E, D, m, policy=EB_POLICY_MAXUTIL, want_load=True,
@@ -247,6 +290,26 @@ def easybalance_pack_weights(desc, kind, n, src, dst, stream=None) -> None:
         ctypes.byref(desc), kind, n, _ptr(src), _ptr(dst), stream))
 
 
+def easybalance_quantize_weights(desc, kind, n, src, q, scales, stream=None, src_dtype=None) -> None:
+    """src_dtype: EB_DTYPE_BF16 or EB_DTYPE_F32; taken from a src tensor's type when not given (fp32, else bf16)."""
+    if src_dtype is None:
+        src_dtype = EB_DTYPE_F32 if str(getattr(src, "dtype", "")) == "torch.float32" else EB_DTYPE_BF16
+    _check("easybalance_quantize_weights", lib().easybalance_quantize_weights(
+        ctypes.byref(desc), kind, n, src_dtype, _ptr(src), _ptr(q), _ptr(scales), stream))
+
+
+def easybalance_packed_fp8_size(desc, kind, n) -> int:
+    out = ctypes.c_size_t(0)
+    _check("easybalance_packed_fp8_size",
+           lib().easybalance_packed_fp8_size(ctypes.byref(desc), kind, n, ctypes.byref(out)))
+    return out.value
+
+
+def easybalance_pack_weights_fp8(desc, kind, n, q, scales, dst, stream=None) -> None:
+    _check("easybalance_pack_weights_fp8", lib().easybalance_pack_weights_fp8(
+        ctypes.byref(desc), kind, n, _ptr(q), _ptr(scales), _ptr(dst), stream))
+
+
 def easybalance_combine(desc, run, n_run, x_list, o, inv, stream=None) -> None:
     xs = _ptr_array(x_list)
     _check("easybalance_combine", lib().easybalance_combine(
@@ -264,6 +327,19 @@ def easybalance_run_pass(desc, N, T, x, gain, Wg, bias, W_gu, W_dn, policy, m, s
                          max_steps=0, record=False, stream=None, placement=None):
     """Returns (n_steps, runsets [n], layers [n][N], step_load [n][D], groups [n],
     layer_loads [N][L][D]) when record, else (n_steps, None, None, None, None, None)."""
+    return _run_pass(None, desc, N, T, x, gain, Wg, bias, None, W_gu, W_dn, policy, m, state, state_bytes, max_steps,
+                     record, stream, placement)
+
+
+def easybalance_run_pass_scored(desc, router, N, T, x, gain, Wg, bias, balance, W_gu, W_dn, policy, m, state,
+                                state_bytes, max_steps=0, record=False, stream=None, placement=None):
+    """easybalance_run_pass under a router from make_router; balance: [L][E] fp32 or None."""
+    return _run_pass(router, desc, N, T, x, gain, Wg, bias, balance, W_gu, W_dn, policy, m, state, state_bytes,
+                     max_steps, record, stream, placement)
+
+
+def _run_pass(router, desc, N, T, x, gain, Wg, bias, balance, W_gu, W_dn, policy, m, state, state_bytes, max_steps,
+              record, stream, placement):
     n = ctypes.c_int32(0)
     if record:
         rs = np.zeros(max_steps, dtype=np.uint64)
@@ -279,10 +355,14 @@ def easybalance_run_pass(desc, N, T, x, gain, Wg, bias, W_gu, W_dn, policy, m, s
     else:
         ptrs = (None, None, None, None, None)
     wg, gu, dn = _ptr_array(Wg), _ptr_array(W_gu), _ptr_array(W_dn)
-    _check("easybalance_run_pass", lib().easybalance_run_pass(
-        ctypes.byref(desc), N, T, _ptr(x), _ptr(gain), wg, _ptr(bias), gu, dn, policy, m,
-        _ptr(state), state_bytes, max_steps if record else 0, ctypes.byref(n), *ptrs,
-        ctypes.byref(placement) if placement is not None else None, stream))
+    tail = (gu, dn, policy, m, _ptr(state), state_bytes, max_steps if record else 0, ctypes.byref(n), *ptrs,
+            ctypes.byref(placement) if placement is not None else None, stream)
+    if router is None:
+        _check("easybalance_run_pass", lib().easybalance_run_pass(
+            ctypes.byref(desc), N, T, _ptr(x), _ptr(gain), wg, _ptr(bias), *tail))
+    else:
+        _check("easybalance_run_pass_scored", lib().easybalance_run_pass_scored(
+            ctypes.byref(desc), ctypes.byref(router), N, T, _ptr(x), _ptr(gain), wg, _ptr(bias), _ptr(balance), *tail))
     k = min(n.value, max_steps) if record else 0
     if not record:
         return n.value, None, None, None, None, None

@@ -25,8 +25,8 @@ int check_desc(const eb_model_desc* d) {
   if (d->L < 1 || d->H < 1 || d->F < 1 || d->E < 1 || d->k < 1 || d->S < 0 || d->D < 1)
     return set_error(EB_ERR_INVALID_ARG, "desc has a non-positive size (L=%d H=%d F=%d E=%d k=%d S=%d D=%d)",
                      d->L, d->H, d->F, d->E, d->k, d->S, d->D);
-  if (d->dtype != EB_DTYPE_F32 && d->dtype != EB_DTYPE_BF16)
-    return set_error(EB_ERR_INVALID_ARG, "dtype %d is not EB_DTYPE_F32/BF16", d->dtype);
+  if (d->dtype != EB_DTYPE_F32 && d->dtype != EB_DTYPE_BF16 && d->dtype != EB_DTYPE_FP8)
+    return set_error(EB_ERR_INVALID_ARG, "dtype %d is not EB_DTYPE_F32/BF16/FP8", d->dtype);
   if (d->k > d->E) return set_error(EB_ERR_INVALID_ARG, "k=%d > E=%d", d->k, d->E);
   if (d->E % d->D != 0) return set_error(EB_ERR_INVALID_ARG, "E=%d not a multiple of D=%d", d->E, d->D);
   if (!(d->rms_eps >= 0.f)) return set_error(EB_ERR_INVALID_ARG, "rms_eps must be >= 0");
@@ -34,12 +34,14 @@ int check_desc(const eb_model_desc* d) {
   if (d->H % 256 != 0) return set_error(EB_ERR_UNSUPPORTED, "H=%d is not a multiple of 256", d->H);
   if (d->F % 128 != 0) return set_error(EB_ERR_UNSUPPORTED, "F=%d is not a multiple of 128", d->F);
   if (d->E + d->S > 1024) return set_error(EB_ERR_UNSUPPORTED, "E+S=%d > 1024", d->E + d->S);
-  if (d->dtype == EB_DTYPE_BF16 && d->E > 256)
+  if (act_dtype(d->dtype) == EB_DTYPE_BF16 && d->E > 256)
     return set_error(EB_ERR_UNSUPPORTED, "bf16 router supports E <= 256 (E=%d)", d->E);
   if (d->k + d->S > kMaxSlots) return set_error(EB_ERR_UNSUPPORTED, "k+S=%d > %d", d->k + d->S, kMaxSlots);
   if (d->L > EB_MAX_LAYERS) return set_error(EB_ERR_UNSUPPORTED, "L=%d > %d", d->L, EB_MAX_LAYERS);
   if (d->dtype == EB_DTYPE_BF16 && 2LL * d->F * d->H * 2 >= (1LL << 31))
     return set_error(EB_ERR_UNSUPPORTED, "an expert's gate/up matrix (2F x H bf16) must be < 2 GiB");
+  if (d->dtype == EB_DTYPE_FP8 && 2LL * d->F * d->H >= (1LL << 31))
+    return set_error(EB_ERR_UNSUPPORTED, "an expert's gate/up matrix (2F x H e4m3) must be < 2 GiB");
   if ((long)d->L * (d->E + d->S) > 15360)
     return set_error(EB_ERR_UNSUPPORTED, "L*(E+S)=%ld > 15360", (long)d->L * (d->E + d->S));
   return EB_OK;
@@ -69,8 +71,13 @@ StepShape step_shape(const eb_model_desc& d, int n_run, const int32_t* T) {
 }
 
 struct WsLayout {
-  size_t hist, chunk_base, offsets, tiles, work_ctr, partial, a_perm, h, total;
+  size_t hist, chunk_base, offsets, tiles, work_ctr, partial, a_perm, h;
+  size_t perm, qa, sa, sh;  // 8-bit stacks
+  size_t total;
 };
+
+// Bytes of the exponents of `rows` rows of K columns (Fp8Problem).
+size_t exponent_bytes(long long rows, int K) { return (size_t)((K + 511) / 512) * (size_t)rows * 4; }
 
 WsLayout ws_layout(const eb_model_desc& d, const StepShape& s, const eb_step_views* v) {
   const size_t eb = d.dtype == EB_DTYPE_BF16 ? 2 : 4;
@@ -87,10 +94,32 @@ WsLayout ws_layout(const eb_model_desc& d, const StepShape& s, const eb_step_vie
   w.tiles = take(sizeof(int4) * (size_t)(s.max_tiles > 0 ? s.max_tiles : 1));
   w.work_ctr = take(sizeof(int32_t) * kWorkWords);
   w.partial = down_ksplit(d.dtype, d.F) > 1 ? take(sizeof(float) * 2 * (size_t)s.P * d.H) : 0;
+  if (d.dtype == EB_DTYPE_FP8) {
+    w.perm = (v && v->perm) ? 0 : take(sizeof(int32_t) * (size_t)s.P);
+    w.qa = take((size_t)s.tokens * d.H);
+    w.sa = take(exponent_bytes(s.tokens, d.H));
+    w.h = take((size_t)s.P * d.F);
+    w.sh = take(exponent_bytes(s.P, d.F));
+    w.total = off;
+    return w;
+  }
   w.a_perm = (v && v->a_perm) ? 0 : take(eb * (size_t)s.P * d.H);
   w.h = (v && v->h) ? 0 : take(eb * (size_t)s.P * d.F);
   w.total = off;
   return w;
+}
+
+// Limits on a step's rows: 32-bit pair numbers and, on 8-bit stacks, 32-bit
+// offsets into the quantised activations and the exponents.
+int check_tokens(const eb_model_desc& d, long long tokens) {
+  const long long P = tokens * (d.k + d.S), most = 0x7fffffffLL;
+  if (P > most) return set_error(EB_ERR_UNSUPPORTED, "step has %lld pairs (> 2^31-1)", P);
+  if (d.dtype == EB_DTYPE_FP8 && tokens * d.H > most)
+    return set_error(EB_ERR_UNSUPPORTED, "8-bit step of %lld tokens: their activations (%lld bytes) exceed 2^31-1",
+                     tokens, tokens * d.H);
+  if (d.dtype == EB_DTYPE_FP8 && (long long)exponent_bytes(P, d.F) > most)
+    return set_error(EB_ERR_UNSUPPORTED, "8-bit step of %lld pairs: their exponents exceed 2^31-1 bytes", P);
+  return EB_OK;
 }
 
 int check_run(const eb_model_desc& d, int32_t n_run, const eb_work* run, bool need_idx) {
@@ -108,9 +137,7 @@ int check_run(const eb_model_desc& d, int32_t n_run, const eb_work* run, bool ne
       return set_error(EB_ERR_INVALID_ARG, "run[%d] has a NULL a/idx/w pointer", i);
     tokens += r.T;
   }
-  if (tokens * (d.k + d.S) > 0x7fffffffLL)
-    return set_error(EB_ERR_UNSUPPORTED, "step has %lld pairs (> 2^31-1)", tokens * (d.k + d.S));
-  return EB_OK;
+  return check_tokens(d, tokens);
 }
 
 RunTable make_run_table(const eb_model_desc& d, int32_t n_run, const eb_work* run,
@@ -142,12 +169,38 @@ int hip_status(hipError_t e, const char* what) {
   return set_error(EB_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+// Body of easybalance_route (router NULL) and easybalance_route_scored.
+int route_common(const eb_model_desc* desc, const eb_router* router, int32_t layer, int32_t T, const float* x,
+                 const float* gain, const void* Wg, const float* bias, const float* balance, void* a_out,
+                 float* logits_out, int32_t* idx_out, float* w_out, int32_t* counts_out, void* stream) {
+  int rc = check_desc(desc);
+  if (rc) return rc;
+  if (router && (rc = check_router(router, desc->E, desc->k))) return rc;
+  if (layer < 0 || layer >= desc->L)
+    return set_error(EB_ERR_INVALID_ARG, "layer=%d outside [0, %d)", layer, desc->L);
+  if (T < 0) return set_error(EB_ERR_INVALID_ARG, "T=%d < 0", T);
+  if (counts_out == nullptr) return set_error(EB_ERR_INVALID_ARG, "counts_out is NULL");
+  if (T > 0 && (x == nullptr || gain == nullptr || Wg == nullptr || bias == nullptr ||
+                a_out == nullptr || idx_out == nullptr || w_out == nullptr))
+    return set_error(EB_ERR_INVALID_ARG, "a required route pointer is NULL");
+  if (T > 0 && logits_out == nullptr && router)
+    return set_error(EB_ERR_INVALID_ARG, "logits_out is NULL, but the choice of experts reads the logits back");
+  if (T > 0 && logits_out == nullptr && route_logits_required(*desc))
+    return set_error(EB_ERR_INVALID_ARG,
+                     "logits_out is NULL, but this stack's top-k reads the logits back (fp32, E=%d, H=%d)",
+                     desc->E, desc->H);
+  return hip_status(launch_route(*desc, router, T, x, gain, Wg, bias, balance, a_out, logits_out, idx_out, w_out,
+                                 counts_out, static_cast<hipStream_t>(stream)),
+                    "route launch");
+}
+
 // A step's buffers carved from its workspace (laid out for shape sh); views
 // that the caller provides replace their workspace slots.
 struct StepWs {
   StepBuffers b;
   float* partial;
   void* h;
+  uint8_t *qa, *sa, *sh;   // 8-bit stacks
 };
 
 StepWs carve_step(const eb_model_desc& d, const StepShape& sh, const eb_step_views* views, void* ws,
@@ -164,6 +217,17 @@ StepWs carve_step(const eb_model_desc& d, const StepShape& sh, const eb_step_vie
   b.max_tiles = sh.max_tiles;
   b.perm = views ? views->perm : nullptr;
   b.inv = inv;
+  w.qa = w.sa = w.sh = nullptr;
+  if (d.dtype == EB_DTYPE_FP8) {
+    if (b.perm == nullptr) b.perm = reinterpret_cast<int32_t*>(base + L.perm);
+    b.a_perm = nullptr;
+    w.partial = nullptr;
+    w.qa = base + L.qa;
+    w.sa = base + L.sa;
+    w.h = base + L.h;
+    w.sh = base + L.sh;
+    return w;
+  }
   b.a_perm = (views && views->a_perm) ? views->a_perm : base + L.a_perm;
   w.partial = L.partial ? reinterpret_cast<float*>(base + L.partial) : nullptr;
   w.h = (views && views->h) ? views->h : base + L.h;
@@ -188,11 +252,42 @@ int run_gemms(const eb_model_desc& d, const StepShape& sh, const StepWs& w, cons
   gp.ksplit = 1;
   gp.partial = nullptr;
   int rc;
+  if (d.dtype == EB_DTYPE_FP8) {
+    Fp8Problem q{gp, (int32_t)sh.tokens, d.k + d.S, w.b.perm, w.qa, w.sa, static_cast<uint8_t*>(w.h), w.sh};
+    if ((rc = hip_status(launch_gateup_fp8(q, wt, s), "gate/up GEMM"))) return rc;
+    q.g.work_ctr = w.b.work_ctr + kWorkDown;
+    return hip_status(launch_down_fp8(q, wt, o, s), "down GEMM");
+  }
   if ((rc = hip_status(launch_gateup(d.dtype, gp, wt, w.b.a_perm, w.h, s), "gate/up GEMM"))) return rc;
   gp.work_ctr = w.b.work_ctr + kWorkDown;
   gp.ksplit = down_ksplit(d.dtype, d.F);
   gp.partial = w.partial;
   return hip_status(launch_down(d.dtype, gp, wt, w.h, o, s, sum_halves), "down GEMM");
+}
+
+// n matrices of an 8-bit stack: rows, columns, bytes of the values and of the scales.
+struct Fp8Shape {
+  int N, K;
+  size_t values, scales;
+};
+
+int fp8_shape(const eb_model_desc* d, int32_t kind, int32_t n, Fp8Shape* w) {
+  const int rc = check_desc(d);
+  if (rc) return rc;
+  if (d->dtype != EB_DTYPE_FP8) return set_error(EB_ERR_INVALID_ARG, "dtype %d is not EB_DTYPE_FP8", d->dtype);
+  if (kind != EB_WEIGHTS_GATE_UP && kind != EB_WEIGHTS_DOWN)
+    return set_error(EB_ERR_INVALID_ARG, "kind %d is not EB_WEIGHTS_GATE_UP/DOWN", kind);
+  if (n < 0) return set_error(EB_ERR_INVALID_ARG, "n=%d < 0", n);
+  w->N = kind == EB_WEIGHTS_GATE_UP ? 2 * d->F : d->H;
+  w->K = kind == EB_WEIGHTS_GATE_UP ? d->H : d->F;
+  w->values = (size_t)n * w->N * w->K;
+  w->scales = (size_t)n * (w->N / 128) * (w->K / 128) * sizeof(float);
+  return EB_OK;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
 }
 
 // ---- kernel timing ---------------------------------------------------------
@@ -233,6 +328,10 @@ int enqueue_step_dev(const eb_model_desc& d, int N, int T, const RunTable* rt, c
   int rc;
   if ((rc = hip_status(launch_permute_dev(d, rt, N, T, w.b, s), "permute")))
     return rc;
+  if (d.dtype == EB_DTYPE_FP8 &&
+      (rc = hip_status(launch_quantize_rows_dev(rt, d.H, (int)sh.tokens, w.qa, reinterpret_cast<uint32_t*>(w.sa), s),
+                       "quantisation")))
+    return rc;
   // a split-K down GEMM leaves its two fp32 halves for the combine, which
   // rounds their sum as the split-K sum kernel would (o is not stored)
   const bool fuse = w.partial != nullptr;
@@ -241,7 +340,31 @@ int enqueue_step_dev(const eb_model_desc& d, int N, int T, const RunTable* rt, c
     return hip_status(
         launch_combine_split_dev(rt, d.k + d.S, (int)sh.tokens, w.partial, (long long)sh.P * d.H, inv, s),
         "combine");
-  return hip_status(launch_combine_dev(rt, d.k + d.S, (int)sh.tokens, d.dtype, o, inv, s), "combine");
+  return hip_status(launch_combine_dev(rt, d.k + d.S, (int)sh.tokens, act_dtype(d.dtype), o, inv, s), "combine");
+}
+
+int check_router(const eb_router* r, int E, int k) {
+  if (r == nullptr) return set_error(EB_ERR_INVALID_ARG, "router is NULL");
+  if (E < 1 || k < 1 || k > E) return set_error(EB_ERR_INVALID_ARG, "E=%d k=%d out of range", E, k);
+  if (r->score != EB_SCORE_SOFTMAX && r->score != EB_SCORE_SIGMOID)
+    return set_error(EB_ERR_INVALID_ARG, "router score %d is not EB_SCORE_SOFTMAX/SIGMOID", r->score);
+  if (r->n_group < 1 || E % r->n_group != 0)
+    return set_error(EB_ERR_INVALID_ARG, "router n_group=%d does not divide E=%d", r->n_group, E);
+  if (r->topk_group < 1 || r->topk_group > r->n_group)
+    return set_error(EB_ERR_INVALID_ARG, "router topk_group=%d outside [1, %d]", r->topk_group, r->n_group);
+  if (r->group_top != 1 && r->group_top != 2)
+    return set_error(EB_ERR_INVALID_ARG, "router group_top=%d is not 1 or 2", r->group_top);
+  const int size = E / r->n_group;
+  if (r->topk_group < r->n_group && r->group_top > size)
+    return set_error(EB_ERR_INVALID_ARG, "router group_top=%d, but groups have %d expert", r->group_top, size);
+  if ((long)r->topk_group * size < k)
+    return set_error(EB_ERR_INVALID_ARG, "k=%d > the %d experts of %d groups", k, r->topk_group * size, r->topk_group);
+  if (r->norm_topk != 0 && r->norm_topk != 1) return set_error(EB_ERR_INVALID_ARG, "router norm_topk must be 0/1");
+  if (!(r->scale - r->scale == 0.f)) return set_error(EB_ERR_INVALID_ARG, "router scale must be finite");
+  if (E > 1024) return set_error(EB_ERR_UNSUPPORTED, "E=%d > 1024", E);
+  if (k > kMaxSlots) return set_error(EB_ERR_UNSUPPORTED, "k=%d > %d", k, kMaxSlots);
+  if (r->n_group > 64) return set_error(EB_ERR_UNSUPPORTED, "router n_group=%d > 64", r->n_group);
+  return EB_OK;
 }
 
 int set_error(int code, const char* fmt, ...) {
@@ -291,22 +414,38 @@ int easybalance_route(const eb_model_desc* desc, int32_t layer, int32_t T, const
                       const float* gain, const void* Wg, const float* bias, void* a_out,
                       float* logits_out, int32_t* idx_out, float* w_out, int32_t* counts_out,
                       void* stream) {
-  int rc = check_desc(desc);
-  if (rc) return rc;
-  if (layer < 0 || layer >= desc->L)
-    return set_error(EB_ERR_INVALID_ARG, "layer=%d outside [0, %d)", layer, desc->L);
+  return route_common(desc, nullptr, layer, T, x, gain, Wg, bias, nullptr, a_out, logits_out, idx_out, w_out,
+                      counts_out, stream);
+}
+
+int easybalance_route_scored(const eb_model_desc* desc, const eb_router* router, int32_t layer, int32_t T,
+                             const float* x, const float* gain, const void* Wg, const float* bias,
+                             const float* balance, void* a_out, float* logits_out, int32_t* idx_out,
+                             float* w_out, int32_t* counts_out, void* stream) {
+  if (router == nullptr) return set_error(EB_ERR_INVALID_ARG, "router is NULL");
+  return route_common(desc, router, layer, T, x, gain, Wg, bias, balance, a_out, logits_out, idx_out, w_out,
+                      counts_out, stream);
+}
+
+int easybalance_select(int32_t T, int32_t E, int32_t k, const eb_router* router, const float* logits,
+                       const float* balance, int32_t* idx_out, float* w_out, int32_t* counts_out, void* stream) {
   if (T < 0) return set_error(EB_ERR_INVALID_ARG, "T=%d < 0", T);
+  const int rc = check_router(router, E, k);
+  if (rc) return rc;
   if (counts_out == nullptr) return set_error(EB_ERR_INVALID_ARG, "counts_out is NULL");
-  if (T > 0 && (x == nullptr || gain == nullptr || Wg == nullptr || bias == nullptr ||
-                a_out == nullptr || idx_out == nullptr || w_out == nullptr))
-    return set_error(EB_ERR_INVALID_ARG, "a required route pointer is NULL");
-  if (T > 0 && logits_out == nullptr && route_logits_required(*desc))
-    return set_error(EB_ERR_INVALID_ARG,
-                     "logits_out is NULL, but this stack's top-k reads the logits back (fp32, E=%d, H=%d)",
-                     desc->E, desc->H);
-  return hip_status(launch_route(*desc, T, x, gain, Wg, bias, a_out, logits_out, idx_out, w_out,
-                                 counts_out, static_cast<hipStream_t>(stream)),
-                    "route launch");
+  if (T > 0 && (logits == nullptr || idx_out == nullptr || w_out == nullptr))
+    return set_error(EB_ERR_INVALID_ARG, "a required select pointer is NULL");
+  RouteBatch rb;
+  memset(&rb, 0, sizeof(rb));
+  rb.n = 1;
+  rb.tok0[1] = T;
+  rb.blk0[1] = T / 32 + (T % 32 != 0);
+  rb.e[0].z = const_cast<float*>(logits);
+  rb.e[0].idx = idx_out;
+  rb.e[0].w = w_out;
+  rb.e[0].counts = counts_out;
+  rb.e[0].balance = balance;
+  return hip_status(launch_select_batch(*router, E, k, rb, static_cast<hipStream_t>(stream)), "select launch");
 }
 
 int easybalance_schedule(int32_t n_pool, const int32_t* pool_ids, const int32_t* counts,
@@ -322,8 +461,12 @@ int easybalance_moe_step_workspace_size(const eb_model_desc* desc, int32_t n_run
   if (rc) return rc;
   if (n_run < 1 || n_run > EB_MAX_RUN || T == nullptr || bytes == nullptr)
     return set_error(EB_ERR_INVALID_ARG, "bad n_run/T/bytes");
-  for (int i = 0; i < n_run; ++i)
+  long long tokens = 0;
+  for (int i = 0; i < n_run; ++i) {
     if (T[i] < 0) return set_error(EB_ERR_INVALID_ARG, "T[%d] < 0", i);
+    tokens += T[i];
+  }
+  if (desc->dtype == EB_DTYPE_FP8 && (rc = check_tokens(*desc, tokens))) return rc;
   *bytes = ws_layout(*desc, step_shape(*desc, n_run, T), nullptr).total;
   return EB_OK;
 }
@@ -357,6 +500,12 @@ int moe_step_common(const eb_model_desc* desc, int32_t n_run, const eb_work* run
     for (int j = 0; j < n_run; ++j) t += run[j].layer == run[i].layer ? run[j].T : 0;
     if (t > sh.layer_tokens) sh.layer_tokens = t;
   }
+  if (d.dtype == EB_DTYPE_FP8) {
+    if (static_scratch)
+      return set_error(EB_ERR_UNSUPPORTED, "8-bit stacks have no static scratch: use easybalance_moe_step, which allocates nothing either");
+    if (views && (views->a_perm || views->h))
+      return set_error(EB_ERR_UNSUPPORTED, "8-bit stacks have no a_perm and h views");
+  }
   if (W_gu == nullptr || W_dn == nullptr) return set_error(EB_ERR_INVALID_ARG, "W_gu/W_dn is NULL");
   WeightTable wt;
   memset(&wt, 0, sizeof(wt));
@@ -384,6 +533,10 @@ int moe_step_common(const eb_model_desc* desc, int32_t n_run, const eb_work* run
 
   const RunTable rt = make_run_table(d, n_run, run, nullptr);
   if ((rc = hip_status(launch_permute(d, rt, w.b, s), "permute"))) return rc;
+  if (d.dtype == EB_DTYPE_FP8 &&
+      (rc = hip_status(launch_quantize_rows(rt, (int)sh.tokens, w.qa, reinterpret_cast<uint32_t*>(w.sa), s),
+                       "quantisation")))
+    return rc;
   return run_gemms(d, sh, w, wt, o_out, s);
 }
 
@@ -407,7 +560,7 @@ int easybalance_combine(const eb_model_desc* desc, int32_t n_run, const eb_work*
   if (tokens == 0) return EB_OK;
   if (o == nullptr || inv == nullptr) return set_error(EB_ERR_INVALID_ARG, "o/inv is NULL");
   const RunTable rt = make_run_table(*desc, n_run, run, x_inout);
-  return hip_status(launch_combine(rt, desc->dtype, o, inv,
+  return hip_status(launch_combine(rt, act_dtype(desc->dtype), o, inv,
                                    static_cast<hipStream_t>(stream)),
                     "combine");
 }
@@ -421,6 +574,8 @@ int easybalance_pack_weights(const eb_model_desc* desc, int32_t kind, int32_t n,
   if (n < 0) return set_error(EB_ERR_INVALID_ARG, "n=%d < 0", n);
   if (n == 0) return EB_OK;
   if (src == nullptr || dst == nullptr) return set_error(EB_ERR_INVALID_ARG, "src/dst is NULL");
+  if (desc->dtype == EB_DTYPE_FP8)
+    return set_error(EB_ERR_INVALID_ARG, "8-bit weights have scales: use easybalance_pack_weights_fp8");
   const int N = kind == EB_WEIGHTS_GATE_UP ? 2 * desc->F : desc->H;
   const int K = kind == EB_WEIGHTS_GATE_UP ? desc->H : desc->F;
   const size_t bytes = (size_t)n * N * K * (desc->dtype == EB_DTYPE_BF16 ? 2 : 4);
@@ -430,6 +585,56 @@ int easybalance_pack_weights(const eb_model_desc* desc, int32_t kind, int32_t n,
   return hip_status(launch_pack_weights(desc->dtype, kind == EB_WEIGHTS_GATE_UP, n, N, K, desc->F, src,
                                         dst, static_cast<hipStream_t>(stream)),
                     "pack_weights");
+}
+
+int easybalance_packed_fp8_size(const eb_model_desc* desc, int32_t kind, int32_t n, size_t* bytes) {
+  Fp8Shape w;
+  const int rc = fp8_shape(desc, kind, n, &w);
+  if (rc) return rc;
+  if (bytes == nullptr) return set_error(EB_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = w.values + w.scales;
+  return EB_OK;
+}
+
+int easybalance_pack_weights_fp8(const eb_model_desc* desc, int32_t kind, int32_t n, const void* q,
+                                 const float* scales, void* dst, void* stream) {
+  Fp8Shape w;
+  const int rc = fp8_shape(desc, kind, n, &w);
+  if (rc) return rc;
+  if (n == 0) return EB_OK;
+  if (q == nullptr || scales == nullptr || dst == nullptr)
+    return set_error(EB_ERR_INVALID_ARG, "q/scales/dst is NULL");
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(dst)) % 16 != 0 ||
+      reinterpret_cast<uintptr_t>(scales) % 4 != 0)
+    return set_error(EB_ERR_INVALID_ARG, "q/dst not 16-byte or scales not 4-byte aligned");
+  if (overlap(q, w.values, dst, w.values + w.scales) || overlap(scales, w.scales, dst, w.values + w.scales))
+    return set_error(EB_ERR_INVALID_ARG, "q or scales and dst overlap");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  // the bf16 block layout on two 8-bit values at a time
+  hipError_t e = launch_pack_weights(EB_DTYPE_BF16, kind == EB_WEIGHTS_GATE_UP, n, w.N, w.K / 2, desc->F, q, dst, s);
+  if (e == hipSuccess) e = launch_copy_scales(scales, static_cast<uint8_t*>(dst) + w.values, w.scales, s);
+  return hip_status(e, "pack_weights_fp8");
+}
+
+int easybalance_quantize_weights(const eb_model_desc* desc, int32_t kind, int32_t n, int32_t src_dtype,
+                                 const void* src, void* q, float* scales, void* stream) {
+  Fp8Shape w;
+  const int rc = fp8_shape(desc, kind, n, &w);
+  if (rc) return rc;
+  if (src_dtype != EB_DTYPE_F32 && src_dtype != EB_DTYPE_BF16)
+    return set_error(EB_ERR_INVALID_ARG, "src_dtype %d is not EB_DTYPE_F32/BF16", src_dtype);
+  if (n == 0) return EB_OK;
+  if (src == nullptr || q == nullptr || scales == nullptr)
+    return set_error(EB_ERR_INVALID_ARG, "src/q/scales is NULL");
+  const size_t bytes = w.values * (src_dtype == EB_DTYPE_BF16 ? 2 : 4);
+  if (reinterpret_cast<uintptr_t>(src) % 16 != 0 || reinterpret_cast<uintptr_t>(q) % 8 != 0 ||
+      reinterpret_cast<uintptr_t>(scales) % 4 != 0)
+    return set_error(EB_ERR_INVALID_ARG, "src not 16-byte, q not 8-byte or scales not 4-byte aligned");
+  if (overlap(src, bytes, q, w.values) || overlap(src, bytes, scales, w.scales) ||
+      overlap(q, w.values, scales, w.scales))
+    return set_error(EB_ERR_INVALID_ARG, "src, q and scales overlap");
+  return hip_status(launch_quantize_blocks(src_dtype, n, w.N, w.K, src, q, scales, static_cast<hipStream_t>(stream)),
+                    "quantize_weights");
 }
 
 int easybalance_profile_begin(uint32_t kernel_mask) {

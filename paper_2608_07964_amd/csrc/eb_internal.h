@@ -66,9 +66,31 @@ struct GroupedProblem {
   float* partial;                          // ksplit 2: [2][P][N] fp32 partial sums
 };
 
+// Storage type of everything but the experts: an 8-bit stack's activations,
+// outputs and router weights are bf16.
+inline int act_dtype(int dtype) { return dtype == EB_DTYPE_FP8 ? EB_DTYPE_BF16 : dtype; }
+
+// Descriptor norm_topk of a routing launch that stops at the logits (the picks
+// follow in launches of their own).
+constexpr int kLogitsOnly = -1;
+
 // K split of the down GEMM: two halves for long K (a rule on the shape only,
 // so every schedule computes a row the same way).
 inline int down_ksplit(int dtype, int F) { return dtype == EB_DTYPE_BF16 && F >= 8192 ? 2 : 1; }
+
+// The same for an 8-bit stack: the tokens' quantised activations, read through
+// the grouping, and the quantised h.  Scales are exponents (E8M0), one byte per
+// row and 128 columns, four columns' blocks to a word: byte
+// ((block / 4) * rows + row) * 4 + block % 4.
+struct Fp8Problem {
+  GroupedProblem g;
+  int32_t tokens, slots;                   // tokens the buffers hold; k + S
+  const int32_t* perm;                     // [P] pair at each grouped position
+  const uint8_t* qa;                       // [tokens][H]
+  const uint8_t* sa;                       // [ceil(H / 512)][tokens][4]
+  uint8_t* h;                              // [P][F]
+  uint8_t* sh;                             // [ceil(F / 512)][P][4]
+};
 
 // Step counters: one 128-byte line per XCD holding its work counter of the
 // gate/up launch, that of its share of the row blocks set aside (kWorkTail
@@ -113,6 +135,7 @@ struct RouteEntry {
   int32_t* idx;
   float* w;
   int32_t* counts;
+  const float* balance;  // [E] bias of the choice under a router, or null
 };
 struct RouteBatch {
   int32_t n;
@@ -148,6 +171,7 @@ struct DevPassArgs {
   int32_t* counts;
   const float* gain;             // [L][H]
   const float* bias;             // [L][E]
+  const float* balance;          // [L][E] under a router, or NULL
   const void* Wg[EB_MAX_LAYERS]; // router weights of each layer
   DevPassState* state;
   RunTable* rt;                  // the step's run table
@@ -177,7 +201,9 @@ struct TailRule {
 };
 
 // ---- launchers (return hipError_t of the launch) ---------------------------
-hipError_t launch_route_batch(const eb_model_desc& d, const RouteBatch& rb, hipStream_t s);
+// router: null, or what the picks go by instead of the descriptor's softmax
+// (the entries' z must then be stored).
+hipError_t launch_route_batch(const eb_model_desc& d, const eb_router* router, const RouteBatch& rb, hipStream_t s);
 // A batch table in device memory (written by the device-side scheduler);
 // grids cover max_entries entries of T tokens.  Only for stacks whose
 // routing needs no launch per entry (route_batch_device_ok).
@@ -185,11 +211,15 @@ bool route_batch_device_ok(const eb_model_desc& d);
 // Whether the top-k of this stack reads the logits back from global memory
 // (fp32 stacks off the one-workgroup-per-token path), so z must be stored.
 bool route_logits_required(const eb_model_desc& d);
-hipError_t launch_route_batch_dev(const eb_model_desc& d, const RouteBatch* rb, int max_entries, int T,
-                                  hipStream_t s);
-hipError_t launch_route(const eb_model_desc& d, int T, const float* x, const float* gain,
-                        const void* Wg, const float* bias, void* a_out, float* logits,
+hipError_t launch_route_batch_dev(const eb_model_desc& d, const eb_router* router, const RouteBatch* rb,
+                                  int max_entries, int T, hipStream_t s);
+hipError_t launch_route(const eb_model_desc& d, const eb_router* router, int T, const float* x, const float* gain,
+                        const void* Wg, const float* bias, const float* balance, void* a_out, float* logits,
                         int32_t* idx, float* w, int32_t* counts, hipStream_t s);
+// The picks of a batch from its entries' logits z (select.hip).
+hipError_t launch_select_batch(const eb_router& p, int E, int k, const RouteBatch& rb, hipStream_t s);
+hipError_t launch_select_batch_dev(const eb_router& p, int E, int k, const RouteBatch* rb, int max_entries, int T,
+                                   hipStream_t s);
 
 // Workspace buffers of one step (see the workspace layout in api.cpp).
 struct StepBuffers {
@@ -199,9 +229,9 @@ struct StepBuffers {
   int4* tiles;
   int32_t* work_ctr;       // [kWorkWords]
   int32_t max_tiles;
-  int32_t* perm;           // or null: nothing in a step reads it, it is for callers that ask
+  int32_t* perm;           // or null: only an 8-bit step reads it, else it is for callers that ask
   int32_t* inv;
-  void* a_perm;
+  void* a_perm;            // or null (8-bit steps): no rows are gathered
 };
 
 // Grouping of a step: perm, inv, offsets, tile list, a_perm; work counters
@@ -227,6 +257,16 @@ hipError_t launch_gateup(int dtype, const GroupedProblem& p, const WeightTable& 
 // is not written (launch_combine_split_dev reads them).
 hipError_t launch_down(int dtype, const GroupedProblem& p, const WeightTable& wt,
                        const void* h, void* o, hipStream_t s, bool sum_halves = true);
+
+// 8-bit stacks: h from qa, o (bf16) from h (gemm_fp8.hip), and what quantises
+// (quant8.hip): a step's tokens (sa's rows: `tokens`), n matrices N x K.
+hipError_t launch_gateup_fp8(const Fp8Problem& p, const WeightTable& wt, hipStream_t s);
+hipError_t launch_down_fp8(const Fp8Problem& p, const WeightTable& wt, void* o, hipStream_t s);
+hipError_t launch_quantize_rows(const RunTable& rt, int tokens, uint8_t* qa, uint32_t* sa, hipStream_t s);
+hipError_t launch_quantize_rows_dev(const RunTable* rt, int H, int tokens, uint8_t* qa, uint32_t* sa, hipStream_t s);
+hipError_t launch_copy_scales(const float* src, void* dst, size_t bytes, hipStream_t s);
+hipError_t launch_quantize_blocks(int src_dtype, int n, int N, int K, const void* src, void* q, float* scales,
+                                  hipStream_t s);
 
 hipError_t launch_combine(const RunTable& rt, int dtype, const void* o, const int32_t* inv,
                           hipStream_t s);
@@ -254,6 +294,8 @@ int moe_step_common(const eb_model_desc* desc, int32_t n_run, const eb_work* run
 int schedule_impl(int32_t n_pool, const int32_t* pool_ids, const int32_t* counts, int32_t E,
                   int32_t D, int32_t m, int32_t policy, uint64_t* runset_mask,
                   int64_t* step_load, const int32_t* pool_layers, const eb_placement* placement);
+// Descriptor and router checks of the entry points (api.cpp).
+int check_router(const eb_router* r, int E, int k);
 // Checks a placement against the model's L, E, D (EB_OK or EB_ERR_INVALID_ARG).
 int check_placement(const eb_placement* p, int L, int E, int D);
 // out[d] += pairs of counts[E] that device d carries at `layer` (placement

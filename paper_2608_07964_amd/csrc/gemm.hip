@@ -1034,7 +1034,7 @@ __global__ __launch_bounds__(256) void pack_bf16_kernel(const uint4* __restrict_
 
 }  // namespace
 
-int gemm_bm(int dtype) { return dtype == EB_DTYPE_BF16 ? BM : FBM; }
+int gemm_bm(int dtype) { return dtype == EB_DTYPE_F32 ? FBM : BM; }
 
 // Row blocks to set aside for the end of a launch (see ItemQueue): one and a
 // half gate/up items per workgroup (the down launch has the same list: 1.1
@@ -1050,7 +1050,7 @@ int gemm_bm(int dtype) { return dtype == EB_DTYPE_BF16 ? BM : FBM; }
 // them, 346 without; a whole pass of that stack, its nine down launches 4.93
 // ms, 4.66 with the rule of ItemQueue as well).
 TailRule gemm_tail(int dtype, int F) {
-  if (dtype != EB_DTYPE_BF16) return TailRule{0, 0};
+  if (dtype == EB_DTYPE_F32) return TailRule{0, 0};
   const int nsub = F / (BN / 2);
   return TailRule{(384 + nsub - 1) / nsub, down_ksplit(dtype, F) > 1 ? CfgSkinny::BM : BM / 2};
 }

@@ -1,0 +1,608 @@
+// Grouped expert GEMMs of 8-bit stacks (EB_DTYPE_FP8): weights in e4m3 with one
+// fp32 scale for each 128 x 128 block, activations in e4m3 with a power-of-two
+// scale for each row's block of 128 columns.
+//
+//   y[r][n] = sum_b sa[r][b] sw[n / 128][b] sum_{k in block b} qa[r][k] qw[n][k]
+//   gate/up: h = SiLU(y_gate) * y_up in fp32, quantised by row and 128 columns
+//   down:    o = bf16(y)
+//
+// The items, their order and the weight layout are those of the bf16 kernels
+// (gemm.hip): an item is up to 256 rows x 256 weight rows, a K stage is 128
+// bytes of every row, here one whole scale block.
+// v_mfma_scale_f32_32x32x64_f8f6f4 takes 64 cycles for 64 bytes of K where the
+// bf16 instruction takes 32 for 32: a stage costs the same matrix cycles and
+// holds twice the products, so the rings, the issue order and the waits carry
+// over.
+//
+// Scales.  The instruction takes a power of two (a biased exponent) per row of
+// each operand.  The activations' scales are powers of two, so theirs go there
+// as they are.  A weight scale sw = 2^x m with m in [1, 2) is split: 2^x goes to
+// the instruction, and the accumulator is kept in units of the current block's
+// m, that is, before block b it is multiplied by m[b-1] / m[b] (one v_mul per
+// accumulator and stage, between the matrix instructions), and by the last m at
+// the end.  This costs no registers (a product per block added in fp32 would
+// need a second set of accumulators) and nothing at all where every scale is a
+// power of two: the ratio is 1 and the item runs without the multiplies.  Its
+// rounding is 2 K/128 half ulps, relative, at worst: as much as the sum's own.
+//
+// Every output accumulates its blocks in ascending order, whatever tile or
+// group its row sits in: rows give the same bits in every schedule.
+#include "eb_internal.h"
+#include "eb_numeric.h"
+#include "gemm_items.h"
+#include "quant8.h"
+
+namespace eb {
+namespace {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// Tiles as in gemm.hip, in bytes: a stage is 128 bytes of K of every row.
+constexpr int BN = 256, BKB = 128;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kBLoads = BN / (8 * kWaves);       // 8-row B loads per wave per stage
+
+template <int BM_, int WM_, int SA_, int SB_>
+struct TileCfg {
+  static constexpr int BM = BM_;
+  static constexpr int WM = WM_, WN = kWaves / WM_;
+  static constexpr int SA = SA_, SB = SB_;
+  static constexpr int TM = BM / WM, TN = BN / WN;
+  static constexpr int MB = TM / 32, NB = TN / 32;
+  static constexpr int A_LOADS = BM / (8 * kWaves);
+  static constexpr int A_BYTES = BM * BKB, B_BYTES = BN * BKB;
+  static constexpr int B_RING = SA * A_BYTES;
+  static constexpr int LDS = SA * A_BYTES + SB * B_BYTES;
+  static_assert(MB >= 1 && NB == 2 && A_LOADS >= 1, "tile shape");
+  static_assert(SA >= 2 && (SB == SA || SB == SA + 1), "ring depths");
+};
+using CfgBig = TileCfg<256, 2, 2, 3>;
+using CfgMid = TileCfg<128, 2, 3, 3>;
+using CfgSkinny = TileCfg<64, 2, 4, 4>;
+constexpr int cmax(int a, int b) { return a > b ? a : b; }
+constexpr int kLds = cmax(cmax(CfgBig::LDS, CfgMid::LDS), CfgSkinny::LDS);
+static_assert(kLds <= 160 * 1024, "LDS budget");
+constexpr int BM = CfgBig::BM;
+// LDS bytes of the gate/up epilogue: the item's quantised rows, the rows'
+// largest values per wavefront column, and the next item's index.
+constexpr int kTileLds = BM * 128, kMaxLds = kTileLds, kNextLds = kMaxLds + 4 * BM * 4;
+
+// An item's loads.  A rows come from anywhere (gate/up: the token of the
+// grouped position), so every A load has its own lane offset; a row past the
+// item's end has one past the buffer's end, which reads zeros.
+struct KLoop {
+  uint8_t* smem;
+  __amdgpu_buffer_rsrc_t ra, rb, rs;  // A rows, the expert's packed weights, the activations' scales
+  int a_lane[4];                   // per-lane A byte offset of load j (row and swizzled chunk)
+  int s_lane[4];                   // per-lane byte offset of the scales of fragment row block mb
+  int s_stride;                    // bytes from one four-block group of scales to the next
+  int b_lane, b_tile, b_stage;     // as in gemm.hip
+  int lds_a_load, lds_b_load, lds_a, lds_b;
+  int sw, nk, khalf;
+  const float* wscale[2];          // the two 32-row weight blocks' scales, one per K block
+};
+
+template <class C>
+struct Frags {
+  intx8 a[C::MB], b[C::NB];
+};
+
+__device__ __forceinline__ void load16_lds(__amdgpu_buffer_rsrc_t r, uint8_t* lds, int voff, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 16, voff, soff, 0, 0);
+}
+template <class C>
+__device__ __forceinline__ void load_a(const KLoop& L, int s, int slot, int j) {
+  load16_lds(L.ra, L.smem + slot * C::A_BYTES + L.lds_a_load + j * 8 * BKB, L.a_lane[j], s * BKB);
+}
+template <class C>
+__device__ __forceinline__ void load_b(const KLoop& L, int s, int slot, int j) {
+  load16_lds(L.rb, L.smem + C::B_RING + slot * C::B_BYTES + L.lds_b_load + j * 8 * BKB, L.b_lane,
+             L.b_tile + s * L.b_stage + j * 1024);
+}
+
+// Loads in flight at the waits: stage t's A loads and the first of its four B
+// loads go out right after the barrier of step t-SA resp. t-SB, A first, the
+// other three B loads in the first half of the step after that (the order of
+// gemm.hip, whose counts these are).
+template <class C>
+struct LoadOrder {
+  static constexpr int after_stage0() {
+    int n = 0;
+    bool after = false;
+    for (int j = -C::SB; j < 0; ++j) {
+      if (j + C::SA >= 0) {
+        if (after) n += C::A_LOADS;
+        if (j + C::SA == 0 && C::SB == C::SA + 1) after = true;
+      }
+      if (j + C::SB >= 0) {
+        if (after) n += 1;
+        if (j + 1 < 0) {
+          if (after) n += kBLoads - 1;
+          if (j + C::SB == 0 && C::SB == C::SA) after = true;
+        }
+      }
+    }
+    return n;
+  }
+  static constexpr int after_next() {
+    return C::SB == C::SA ? (C::SA - 2) * (C::A_LOADS + kBLoads)
+                          : kBLoads + (C::SA - 2) * (C::A_LOADS + kBLoads);
+  }
+  static_assert(after_next() < 64 && after_stage0() < 64, "vmcnt range");
+};
+
+// Half h (64 bytes of K) of a fragment row: 16-byte chunks 4 h + khalf and
+// 4 h + 2 + khalf, the same for both operands, so the products pair up.
+template <class C>
+__device__ __forceinline__ const uint8_t* frag_a(const KLoop& L, int slot, int chunk) {
+  return L.smem + slot * C::A_BYTES + ((chunk + L.khalf) ^ L.sw) * 16 + L.lds_a;
+}
+template <class C>
+__device__ __forceinline__ const uint8_t* frag_b(const KLoop& L, int slot, int chunk) {
+  return L.smem + C::B_RING + slot * C::B_BYTES + ((chunk + L.khalf) ^ L.sw) * 16 + L.lds_b;
+}
+__device__ __forceinline__ intx8 read_frag(const uint8_t* lo, const uint8_t* hi) {
+  const intx4 a = *reinterpret_cast<const intx4*>(lo), b = *reinterpret_cast<const intx4*>(hi);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+struct StepLoads {
+  int a_s, a_slot, b_s, b_slot, b_j0;
+};
+template <class C, int NA>
+__device__ __forceinline__ void step_load(const KLoop& L, const StepLoads& ld, int j) {
+  if (j < NA) load_a<C>(L, ld.a_s, ld.a_slot, j);
+  else load_b<C>(L, ld.b_s, ld.b_slot, ld.b_j0 + j - NA);
+}
+
+// The scales of one stage: weight exponents (uniform), the activations' four
+// next exponents of each row block (the current one in the low byte), and the
+// factors that bring the accumulators to this block's units.
+template <class C>
+struct StageScales {
+  int w[C::NB];
+  int a[C::MB];
+  float ratio[C::NB];
+};
+
+// One half stage in a fixed issue order (as kstep of gemm.hip): its MFMAs run
+// block row by block row with the fragment reads of the next half and the
+// V loads of `ld` between them.  FIRST && SCALED: each accumulator block is
+// brought to the stage's units before its first MFMA.  The weight fragment is
+// the first operand: lane l holds token row l % 32 and weight rows
+// 8 (v / 4) + 4 (l / 32) + v % 4.
+template <class C, int NACT, int NA, int V, bool MUL>
+__device__ __forceinline__ void half_step(const KLoop& L, const Frags<C>& cur, Frags<C>& nxt, int slot_a, int slot_b,
+                                          int h_next, floatx16 (&acc)[C::MB][C::NB], const StageScales<C>& sc,
+                                          const StepLoads& ld) {
+  constexpr int M = NACT * C::NB;
+  constexpr int R = NACT > 0 ? C::NB + NACT : 0;
+  constexpr int OPS = R + V;
+  if constexpr (M == 0) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) step_load<C, NA>(L, ld, j);
+  } else {
+    const uint8_t* a0 = frag_a<C>(L, slot_a, 4 * h_next);
+    const uint8_t* a1 = frag_a<C>(L, slot_a, 4 * h_next + 2);
+    const uint8_t* b0 = frag_b<C>(L, slot_b, 4 * h_next);
+    const uint8_t* b1 = frag_b<C>(L, slot_b, 4 * h_next + 2);
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const int mb = i / C::NB, nb = i % C::NB;
+      if constexpr (MUL) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[mb][nb][v] *= sc.ratio[nb];
+      }
+      acc[mb][nb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(cur.b[nb], cur.a[mb], acc[mb][nb], 0, 0, 0,
+                                                                    sc.w[nb], 0, sc.a[mb]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < OPS; ++j) {
+        if ((j * M) / OPS == i) {
+          if (j < C::NB)
+            nxt.b[j] = read_frag(b0 + j * 32 * BKB, b1 + j * 32 * BKB);
+          else if (j < R)
+            nxt.a[j - C::NB] = read_frag(a0 + (j - C::NB) * 32 * BKB, a1 + (j - C::NB) * 32 * BKB);
+          else
+            step_load<C, NA>(L, ld, j - R);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
+}
+
+// The scales of 64 K blocks of a weight block, one per lane: exponent, mantissa
+// and the ratio to the block before (prev: the mantissa of the block before
+// lane 0's, 0 for the first block of all).
+struct WeightScales {
+  int expo;
+  float ratio, mant;
+};
+__device__ __forceinline__ float scale_word(const float* s, int k0, int nk, int lane) {
+  return s[min(k0 + lane, nk - 1)];
+}
+__device__ __forceinline__ WeightScales weight_scales(float word, float prev, int lane) {
+  const uint32_t u = __float_as_uint(word);
+  WeightScales w;
+  w.expo = (u >> 23) & 0xff;
+  // 0 and subnormal scales count as 2^-127; inf and NaN (exponent 255) make
+  // the instruction's scale NaN
+  w.mant = w.expo == 0 ? 1.f : __uint_as_float((u & 0x7fffffu) | 0x3f800000u);
+  float before = __shfl_up(w.mant, 1, 64);
+  if (lane == 0) before = prev == 0.f ? w.mant : prev;
+  w.ratio = before / w.mant;
+  return w;
+}
+
+// The ring's first loads, in the order of the steps -SB .. -1.
+template <class C>
+__device__ __forceinline__ void prologue(const KLoop& L) {
+  const int last = L.nk - 1;
+#pragma unroll
+  for (int j = -C::SB; j < 0; ++j) {
+    if (j + C::SA >= 0)
+#pragma unroll
+      for (int q = 0; q < C::A_LOADS; ++q) load_a<C>(L, min(j + C::SA, last), j + C::SA, q);
+    if (j + C::SB >= 0) {
+      load_b<C>(L, min(j + C::SB, last), j + C::SB, 0);
+      if (j + 1 < 0)
+#pragma unroll
+        for (int q = 1; q < kBLoads; ++q) load_b<C>(L, min(j + C::SB, last), j + C::SB, q);
+    }
+  }
+}
+
+// One item's K loop after its prologue (see k_loop of gemm.hip for the ring
+// discipline).  NS: 2 where the wavefront's two weight blocks have scales of
+// their own (gate and up), 1 where they share them.  sa: the first four K
+// blocks' exponents of each row block.
+template <class C, int NACT, bool SCALED, int NS>
+__device__ __forceinline__ void k_loop(const KLoop& L, floatx16 (&acc)[C::MB][C::NB], int (&sa)[C::MB],
+                                       WeightScales (&ws)[NS], int lane) {
+  const int nk = L.nk, last = nk - 1;
+  int sn[C::MB];
+#pragma unroll
+  for (int mb = 0; mb < C::MB; ++mb) sn[mb] = 0;
+  int pb_s = min(C::SB - 1, last), pb_slot = C::SB - 1;
+  wait_vm<LoadOrder<C>::after_stage0()>();
+  bar();
+  Frags<C> f[2];
+  if (NACT > 0) {
+#pragma unroll
+    for (int nb = 0; nb < C::NB; ++nb)
+      f[0].b[nb] = read_frag(frag_b<C>(L, 0, 0) + nb * 32 * BKB, frag_b<C>(L, 0, 2) + nb * 32 * BKB);
+#pragma unroll
+    for (int mb = 0; mb < NACT; ++mb)
+      f[0].a[mb] = read_frag(frag_a<C>(L, 0, 0) + mb * 32 * BKB, frag_a<C>(L, 0, 2) + mb * 32 * BKB);
+  }
+  StageScales<C> sc;
+  int ca = 0, cb = 0;
+  for (int kt = 0; kt < nk; ++kt) {
+    if (NACT > 0) {
+      if ((kt & 63) == 0 && kt > 0) {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+          const float prev = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws[n].mant), 63));
+          ws[n] = weight_scales(scale_word(L.wscale[n], kt, nk, lane), prev, lane);
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < C::NB; ++nb) {
+        const int n = nb < NS ? nb : NS - 1;
+        sc.w[nb] = __builtin_amdgcn_readlane(ws[n].expo, kt & 63);
+        sc.ratio[nb] = SCALED ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws[n].ratio), kt & 63)) : 1.f;
+      }
+#pragma unroll
+      for (int mb = 0; mb < NACT; ++mb) sc.a[mb] = sa[mb];
+    }
+    {
+      const StepLoads ld{0, 0, pb_s, pb_slot, 1};
+      half_step<C, NACT, 0, kBLoads - 1, SCALED>(L, f[0], f[1], ca, cb, 1, acc, sc, ld);
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    wait_vm<LoadOrder<C>::after_next()>();
+    bar();
+    // the next four blocks' scales, before this step's ring loads
+    if (NACT > 0 && (kt & 3) == 0) {
+#pragma unroll
+      for (int mb = 0; mb < NACT; ++mb)
+        sn[mb] = __builtin_amdgcn_raw_buffer_load_b32(L.rs, L.s_lane[mb], ((kt >> 2) + 1) * L.s_stride, 0);
+    }
+    pb_s = min(kt + C::SB, last);
+    pb_slot = cb;
+    const int na = ca + 1 == C::SA ? 0 : ca + 1;
+    const int nb = cb + 1 == C::SB ? 0 : cb + 1;
+    {
+      const StepLoads ld{min(kt + C::SA, last), ca, pb_s, pb_slot, 0};
+      half_step<C, NACT, C::A_LOADS, C::A_LOADS + 1, false>(L, f[1], f[0], na, nb, 0, acc, sc, ld);
+    }
+#pragma unroll
+    for (int mb = 0; mb < NACT; ++mb) sa[mb] = (kt & 3) == 3 ? sn[mb] : (int)((uint32_t)sa[mb] >> 8);
+    ca = na;
+    cb = nb;
+  }
+  wait_vm<0>();
+}
+
+template <class C, bool SCALED, int NS>
+__device__ __forceinline__ void k_loop_nact(const KLoop& kl, floatx16 (&acc)[C::MB][C::NB], int (&sa)[C::MB],
+                                            WeightScales (&ws)[NS], int nact, int lane) {
+  if constexpr (C::MB == 4) {
+    switch (nact) {
+      case 4: k_loop<C, 4, SCALED, NS>(kl, acc, sa, ws, lane); break;
+      case 3: k_loop<C, 3, SCALED, NS>(kl, acc, sa, ws, lane); break;
+      case 2: k_loop<C, 2, SCALED, NS>(kl, acc, sa, ws, lane); break;
+      case 1: k_loop<C, 1, SCALED, NS>(kl, acc, sa, ws, lane); break;
+      default: k_loop<C, 0, SCALED, NS>(kl, acc, sa, ws, lane); break;
+    }
+  } else if constexpr (C::MB == 2) {
+    switch (nact) {
+      case 2: k_loop<C, 2, SCALED, NS>(kl, acc, sa, ws, lane); break;
+      case 1: k_loop<C, 1, SCALED, NS>(kl, acc, sa, ws, lane); break;
+      default: k_loop<C, 0, SCALED, NS>(kl, acc, sa, ws, lane); break;
+    }
+  } else {
+    static_assert(C::MB == 1, "tile shape");
+    if (nact == 1) k_loop<C, 1, SCALED, NS>(kl, acc, sa, ws, lane);
+    else k_loop<C, 0, SCALED, NS>(kl, acc, sa, ws, lane);
+  }
+}
+
+// Gate/up epilogue: the item's 128 columns of h are one scale block of the
+// down GEMM.  A lane holds 16 of a row's columns; their largest |h| meets
+// those of the other lanes and wavefront columns through LDS, then the row is
+// quantised, collected in LDS and stored as whole 128-byte lines.
+template <class C>
+__device__ __forceinline__ void epilogue_gateup(const Fp8Problem& p, floatx16 (&acc)[C::MB][C::NB], const float (&m)[2],
+                                                uint8_t* smem, int row0, int row_end, int ni, int wave, int wm, int wn,
+                                                int tm, int nact, int lane) {
+  const int lrow = lane & 31, khalf = lane >> 5;
+  float* mx = reinterpret_cast<float*>(smem + kMaxLds);  // [4 wavefront columns][BM]
+#pragma unroll
+  for (int mb = 0; mb < C::MB; ++mb) {
+    if (mb >= nact) continue;
+    float a = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const float h = swiglu(acc[mb][0][v] * m[0], acc[mb][1][v] * m[1]);
+      acc[mb][0][v] = h;
+      a = fmaxf(a, finite_magnitude(h));
+    }
+    a = fmaxf(a, __shfl_xor(a, 32, 64));
+    if (khalf == 0) mx[wn * BM + wm * tm + mb * 32 + lrow] = a;
+  }
+  bar_lds();
+#pragma unroll
+  for (int mb = 0; mb < C::MB; ++mb) {
+    if (mb >= nact) continue;
+    const int r = wm * tm + mb * 32 + lrow;
+    const float a = fmaxf(fmaxf(mx[r], mx[BM + r]), fmaxf(mx[2 * BM + r], mx[3 * BM + r]));
+    const int e8 = scale_exponent(a);
+    const float inv = inverse_scale(e8);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const floatx16& h = acc[mb][0];
+      const uint32_t q = pack_e4m3x4(h[4 * g] * inv, h[4 * g + 1] * inv, h[4 * g + 2] * inv, h[4 * g + 3] * inv);
+      *reinterpret_cast<uint32_t*>(smem + r * 128 + ((2 * wn + (g >> 1)) ^ (r & 7)) * 16 + (g & 1) * 8 + khalf * 4) = q;
+    }
+    if (wn == 0 && khalf == 0 && row0 + r < row_end)
+      p.sh[((size_t)(ni >> 2) * p.g.P + row0 + r) * 4 + (ni & 3)] = (uint8_t)e8;
+  }
+  bar_lds();
+  const int F = p.g.F, rows = row_end - row0;
+  const int c = lane & 7;
+#pragma unroll
+  for (int i = 0; i < C::BM / 64; ++i) {
+    const int r = (C::BM / 8) * wave + 8 * i + (lane >> 3);
+    if (r < rows)
+      *reinterpret_cast<u32x4*>(p.h + (size_t)(row0 + r) * F + ni * 128 + c * 16) =
+          *reinterpret_cast<const u32x4*>(smem + r * 128 + (c ^ (r & 7)) * 16);
+  }
+}
+
+// Down epilogue: o = bf16(m acc), each wavefront's tile through its own part
+// of the ring so that a store writes whole 128-byte runs of a row.
+template <class C>
+__device__ __forceinline__ void epilogue_down(const Fp8Problem& p, const floatx16 (&acc)[C::MB][C::NB], float m,
+                                              uint8_t* smem, bf16_t* o, int row0, int row_end, int ni, int r0w,
+                                              int wave, int wn, int nact, int lane) {
+  const int N = p.g.H;
+  const int lrow = lane & 31, khalf = lane >> 5;
+  bf16_t* st = reinterpret_cast<bf16_t*>(smem) + wave * (C::TM * C::TN);
+#pragma unroll
+  for (int mb = 0; mb < C::MB; ++mb) {
+    if (mb >= nact) continue;
+    const int r = mb * 32 + lrow;
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx16& c = acc[mb][nb];
+        uint2 v;
+        v.x = pack_bf16x2(c[4 * g] * m, c[4 * g + 1] * m);
+        v.y = pack_bf16x2(c[4 * g + 2] * m, c[4 * g + 3] * m);
+        *reinterpret_cast<uint2*>(st + r * C::TN + swz(r, nb * 4 + g) * 8 + khalf * 4) = v;
+      }
+  }
+  asm volatile("" ::: "memory");  // the reads below are of the bytes written above, as another type
+  const int rows = max(0, min(nact * 32, row_end - row0 - r0w));
+  const __amdgpu_buffer_rsrc_t rc = buffer_rsrc(uniform(o + (size_t)(row0 + r0w) * N), (uint32_t)(rows * N * 2));
+  const int rl = lane / 8, c = lane % 8;
+  int off = (rl * N + ni * BN + wn * C::TN + c * 8) * 2;
+#pragma unroll
+  for (int i = 0; i < C::TM / 8; ++i) {
+    if (i * 8 < nact * 32) {
+      const int r = i * 8 + rl;
+      __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4*>(st + r * C::TN + swz(r, c) * 8), rc, off, 0, 0);
+    }
+    off += 8 * N * 2;
+  }
+}
+
+template <class C, int MODE>
+__device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf16_t* o, const uint8_t* Bbase,
+                                         const float* scales, int row0, int row_end, int ni, int wave, int lane) {
+  const int K = MODE == MODE_GATEUP ? p.g.H : p.g.F;
+  const int n_rows = MODE == MODE_GATEUP ? 2 * p.g.F : p.g.H;
+  const int nk = K / BKB;
+  const int wm = wave / C::WN, wn = wave % C::WN;
+  const int lrow = lane & 31;
+  // rows per wavefront row: the tile's rows split evenly in whole 32-row blocks
+  const int tm = min(C::TM, 32 * ((row_end - row0 + 32 * C::WM - 1) / (32 * C::WM)));
+  const int lr = lane >> 3, lp = lane & 7;
+
+  KLoop kl;
+  kl.smem = smem;
+  kl.rb = buffer_rsrc(Bbase, (uint32_t)n_rows * (uint32_t)K);
+  // row of the A buffer and of the scales that tile row r is
+  auto a_row = [&](int r) {
+    const int row = min(row0 + r, row_end - 1);
+    if constexpr (MODE == MODE_GATEUP) return min(max(p.perm[row] / p.slots, 0), p.tokens - 1);  // grouped positions that no pair maps to hold anything
+    else return row;
+  };
+  const int pieces = (nk + 3) / 4;
+  if constexpr (MODE == MODE_GATEUP) {
+    kl.ra = buffer_rsrc(p.qa, (uint32_t)p.tokens * (uint32_t)K);
+    kl.rs = buffer_rsrc(p.sa, (uint32_t)(pieces * 4) * (uint32_t)p.tokens);
+    kl.s_stride = p.tokens * 4;
+  } else {
+    kl.ra = buffer_rsrc(p.h + (size_t)row0 * K, (uint32_t)(row_end - row0) * (uint32_t)K);
+    kl.rs = buffer_rsrc(p.sh, (uint32_t)(pieces * 4) * (uint32_t)p.g.P);
+    kl.s_stride = p.g.P * 4;
+  }
+  const int ca = lp ^ ((((C::BM / kWaves) * wave + lr) >> 1) & 7);  // swizzle of the wave's first load row; odd j flip bit 2
+#pragma unroll
+  for (int j = 0; j < C::A_LOADS; ++j) {
+    const int r = (C::BM / kWaves) * wave + 8 * j + lr;
+    const int at = MODE == MODE_GATEUP ? a_row(r) : r;
+    kl.a_lane[j] = row0 + r < row_end ? at * K + ((j & 1) ? ca ^ 4 : ca) * 16 : (int)0x80000000;
+  }
+#pragma unroll
+  for (int mb = 0; mb < C::MB; ++mb) kl.s_lane[mb] = a_row(wm * tm + mb * 32 + lrow) * 4;
+  kl.b_lane = lane * 16;
+  kl.b_stage = (n_rows / BN) * (BN * BKB);
+  kl.b_tile = ni * (BN * BKB) + wave * (BN / kWaves) * BKB;
+  kl.lds_a_load = (C::BM / kWaves) * wave * BKB;
+  kl.lds_b_load = (BN / kWaves) * wave * BKB;
+  kl.lds_a = (wm * tm + lrow) * BKB;
+  kl.lds_b = (wn * C::TN + lrow) * BKB;
+  kl.sw = (lrow >> 1) & 7;
+  kl.nk = nk;
+  kl.khalf = lane >> 5;
+  // gate/up: column tile ni is f block ni, whose up rows' block is F/128 later;
+  // down: two 128-row blocks to a column tile, two wavefront columns to a block
+  constexpr int NS = MODE == MODE_GATEUP ? 2 : 1;
+  kl.wscale[0] = scales + (size_t)(MODE == MODE_GATEUP ? ni : 2 * ni + (wn >> 1)) * nk;
+  kl.wscale[1] = MODE == MODE_GATEUP ? kl.wscale[0] + (size_t)(p.g.F / 128) * nk : kl.wscale[0];
+
+  // the scales' first words, before the ring's loads: a wait for those covers them
+  float word[NS];
+  int sa[C::MB];
+#pragma unroll
+  for (int n = 0; n < NS; ++n) word[n] = scale_word(kl.wscale[n], 0, nk, lane);
+#pragma unroll
+  for (int mb = 0; mb < C::MB; ++mb) sa[mb] = __builtin_amdgcn_raw_buffer_load_b32(kl.rs, kl.s_lane[mb], 0, 0);
+  prologue<C>(kl);
+  floatx16 acc[C::MB][C::NB];
+#pragma unroll
+  for (int i = 0; i < C::MB; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NB; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  const int nact = min(tm / 32, max(0, (row_end - (row0 + wm * tm) + 31) / 32));
+  // whether any scale is not a power of two, and the last one's mantissa
+  float m[2] = {1.f, 1.f};
+  bool scaled = false;
+  WeightScales ws[NS];
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    ws[n] = weight_scales(word[n], 0.f, lane);
+    scaled |= __any(ws[n].mant != 1.f);
+    m[n] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws[n].mant), min(nk - 1, 63)));
+    for (int k0 = 64; k0 < nk; k0 += 64) {
+      const WeightScales w = weight_scales(scale_word(kl.wscale[n], k0, nk, lane), 0.f, lane);
+      scaled |= __any(w.mant != 1.f);
+      m[n] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w.mant), min(nk - 1 - k0, 63)));
+    }
+  }
+  if (scaled) k_loop_nact<C, true, NS>(kl, acc, sa, ws, nact, lane);
+  else k_loop_nact<C, false, NS>(kl, acc, sa, ws, nact, lane);
+  bar_lds();  // every wave is done with the ring before it is written again
+  if constexpr (MODE == MODE_GATEUP)
+    epilogue_gateup<C>(p, acc, m, smem, row0, row_end, ni, wave, wm, wn, tm, nact, lane);
+  else
+    epilogue_down<C>(p, acc, m[0], smem, o, row0, row_end, ni, wm * tm, wave, wn, nact, lane);
+}
+
+// Persistent grouped GEMM over the items of the step (see grouped_gemm_bf16).
+template <int MODE>
+__global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, WeightTable wt, bf16_t* __restrict__ o,
+                                                                int n_ntiles) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kLds];
+  // the next item's index passes through the ring, at a place that neither the
+  // epilogues' rows nor (between an item's end and the next prologue) a load uses
+  int* s_next = reinterpret_cast<int*>(smem + (MODE == MODE_GATEUP ? kNextLds : 0));
+  // the LDS ring is written by global->LDS loads the compiler does not see
+  asm volatile("" ::"v"(smem) : "memory");
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  ItemQueue q(p.g, n_ntiles);  // used by thread 0 only
+  const int ES = p.g.E + p.g.S;
+  const size_t mat = (size_t)(MODE == MODE_GATEUP ? 2 : 1) * p.g.F * p.g.H;  // bytes of an expert's matrix
+
+  if (tid == 0) *s_next = q.first();
+  __syncthreads();
+  int it = __builtin_amdgcn_readfirstlane(*s_next);
+  __syncthreads();
+
+  while (it >= 0) {
+    int got = 0;
+    if (tid == 0) got = q.draw();
+    const int4 gd = scalar_record(p.g.tiles, it / n_ntiles);  // key, first row, rows, first m-tile
+    const int mt = (gd.z + BM - 1) / BM;
+    const Tile2 tile = item_tile(it - gd.w * n_ntiles, mt, n_ntiles);
+    // the group's mt m-tiles share its rows evenly (whole 32-row blocks)
+    const int rpt = 32 * ((gd.z + 32 * mt - 1) / (32 * mt));
+    const int row0 = gd.y + tile.mi * rpt, row_end = min(gd.y + gd.z, row0 + rpt);
+    const int layer = gd.x / ES, e = gd.x - layer * ES;
+    const uint8_t* W = static_cast<const uint8_t*>(MODE == MODE_GATEUP ? wt.gu[layer] : wt.dn[layer]);
+    const uint8_t* Bbase = W + e * mat;
+    const float* scales = reinterpret_cast<const float*>(W + ES * mat) + e * (mat / (128 * 128));
+    const int rows = row_end - row0;
+    if (rows > CfgMid::BM)
+      run_item<CfgBig, MODE>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, wave, lane);
+    else if (rows > CfgSkinny::BM)
+      run_item<CfgMid, MODE>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, wave, lane);
+    else
+      run_item<CfgSkinny, MODE>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, wave, lane);
+    if (tid == 0) *s_next = q.settle(got);
+    bar_lds();
+    it = __builtin_amdgcn_readfirstlane(*s_next);
+    bar_lds();  // every thread has read it before the next prologue refills the ring
+  }
+}
+
+}  // namespace
+
+hipError_t launch_gateup_fp8(const Fp8Problem& p, const WeightTable& wt, hipStream_t s) {
+  prof_start(EB_K_GATEUP, s);
+  hipLaunchKernelGGL(grouped_gemm_fp8<MODE_GATEUP>, dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
+                     static_cast<bf16_t*>(nullptr), p.g.F / 128);
+  prof_stop(EB_K_GATEUP, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_down_fp8(const Fp8Problem& p, const WeightTable& wt, void* o, hipStream_t s) {
+  prof_start(EB_K_DOWN, s);
+  hipLaunchKernelGGL(grouped_gemm_fp8<MODE_DOWN>, dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
+                     static_cast<bf16_t*>(o), p.g.H / BN);
+  prof_stop(EB_K_DOWN, s);
+  return hipGetLastError();
+}
+
+}  // namespace eb

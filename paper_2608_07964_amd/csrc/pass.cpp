@@ -40,7 +40,7 @@ struct PassLayout {
 };
 
 PassLayout pass_layout(const eb_model_desc& d, int N, int T) {
-  const size_t eb = d.dtype == EB_DTYPE_BF16 ? 2 : 4;
+  const size_t eb = act_dtype(d.dtype) == EB_DTYPE_BF16 ? 2 : 4;
   const size_t NT = (size_t)N * T, slots = (size_t)(d.k + d.S);
   PassLayout p{};
   size_t off = 0;
@@ -157,13 +157,13 @@ int wait_status(hipStream_t s, uint32_t tag, int steps, PassStatus* out) {
 
 // Algorithm 1 with the Schedule step on the GPU (see the file comment).
 // Inputs as validated by easybalance_run_pass; the layer-0 routing is queued.
-int run_pass_device(const eb_model_desc& d, int N, int T, const PassLayout& P, uint8_t* base, float* x,
+int run_pass_device(const eb_model_desc& d, const eb_router* router, const float* balance, int N, int T, const PassLayout& P, uint8_t* base, float* x,
                     const float* gain, const void* const* Wg, const float* bias,
                     const void* const* W_gu, const void* const* W_dn, int policy, int m,
                     int max_steps, int32_t* n_steps_out, uint64_t* runsets_out, int32_t* layers_out,
                     int64_t* step_load_out, int32_t* groups_out, int32_t* layer_loads_out,
                     const eb_placement* placement, hipStream_t s) {
-  const size_t eb = d.dtype == EB_DTYPE_BF16 ? 2 : 4;
+  const size_t eb = act_dtype(d.dtype) == EB_DTYPE_BF16 ? 2 : 4;
   DevPassArgs A;
   memset(&A, 0, sizeof(A));
   A.N = N;
@@ -188,6 +188,7 @@ int run_pass_device(const eb_model_desc& d, int N, int T, const PassLayout& P, u
   A.counts = reinterpret_cast<int32_t*>(base + P.counts);
   A.gain = gain;
   A.bias = bias;
+  A.balance = balance;
   for (int l = 0; l < d.L; ++l) A.Wg[l] = Wg[l];
   A.state = reinterpret_cast<DevPassState*>(base + P.dstate);
   A.rt = reinterpret_cast<RunTable*>(base + P.drt);
@@ -225,7 +226,7 @@ int run_pass_device(const eb_model_desc& d, int N, int T, const PassLayout& P, u
     if (launch_sched_step(A, s) != hipSuccess) return set_error(EB_ERR_HIP, "scheduler launch");
     if ((rc = enqueue_step_dev(d, N, T, A.rt, wt, ws, o, inv, s))) return rc;
     for (int b = 0; b * kRouteBatch < N; ++b)
-      if (launch_route_batch_dev(d, A.rb + b, std::min(kRouteBatch, N - b * kRouteBatch), T, s) != hipSuccess)
+      if (launch_route_batch_dev(d, router, A.rb + b, std::min(kRouteBatch, N - b * kRouteBatch), T, s) != hipSuccess)
         return set_error(EB_ERR_HIP, "route launch");
     return EB_OK;
   };
@@ -269,35 +270,19 @@ int run_pass_device(const eb_model_desc& d, int N, int T, const PassLayout& P, u
   return EB_OK;
 }
 
-}  // namespace
-}  // namespace eb
-
-using namespace eb;
-
-extern "C" {
-
-int easybalance_pass_state_size(const eb_model_desc* desc, int32_t N, int32_t T, size_t* bytes) {
-  if (desc == nullptr || bytes == nullptr) return set_error(EB_ERR_INVALID_ARG, "desc/bytes is NULL");
-  if (N < 1 || N > EB_MAX_POOL || T < 1) return set_error(EB_ERR_INVALID_ARG, "N=%d T=%d out of range", N, T);
-  size_t wsb = 0;
-  std::vector<int32_t> Ts(N, T);
-  const int rc = easybalance_moe_step_workspace_size(desc, N, Ts.data(), &wsb);
-  if (rc) return rc;
-  *bytes = pass_layout(*desc, N, T).total;
-  return EB_OK;
-}
-
-int easybalance_run_pass(const eb_model_desc* desc, int32_t N, int32_t T, float* x,
-                         const float* gain, const void* const* Wg, const float* bias,
-                         const void* const* W_gu, const void* const* W_dn, int32_t policy,
-                         int32_t m, void* state, size_t state_bytes, int32_t max_steps,
-                         int32_t* n_steps_out, uint64_t* runsets_out, int32_t* layers_out,
-                         int64_t* step_load_out, int32_t* groups_out, int32_t* layer_loads_out,
-                         const eb_placement* placement, void* stream) {
+// Body of easybalance_run_pass (router NULL) and easybalance_run_pass_scored.
+int run_pass_common(const eb_model_desc* desc, const eb_router* router, int32_t N, int32_t T, float* x,
+                    const float* gain, const void* const* Wg, const float* bias, const float* balance,
+                    const void* const* W_gu, const void* const* W_dn, int32_t policy,
+                    int32_t m, void* state, size_t state_bytes, int32_t max_steps,
+                    int32_t* n_steps_out, uint64_t* runsets_out, int32_t* layers_out,
+                    int64_t* step_load_out, int32_t* groups_out, int32_t* layer_loads_out,
+                    const eb_placement* placement, void* stream) {
   size_t need = 0;
   int rc = easybalance_pass_state_size(desc, N, T, &need);
   if (rc) return rc;
   const eb_model_desc& d = *desc;
+  if (router && (rc = check_router(router, d.E, d.k))) return rc;
   if (x == nullptr || gain == nullptr || Wg == nullptr || bias == nullptr || W_gu == nullptr ||
       W_dn == nullptr)
     return set_error(EB_ERR_INVALID_ARG, "a required pass pointer is NULL");
@@ -324,7 +309,7 @@ int easybalance_run_pass(const eb_model_desc* desc, int32_t N, int32_t T, float*
 
   const PassLayout P = pass_layout(d, N, T);
   uint8_t* base = static_cast<uint8_t*>(state);
-  const size_t eb = d.dtype == EB_DTYPE_BF16 ? 2 : 4;
+  const size_t eb = act_dtype(d.dtype) == EB_DTYPE_BF16 ? 2 : 4;
   auto a_of = [&](int j) { return base + P.a + eb * (size_t)j * T * d.H; };
   auto logits_of = [&](int j) { return reinterpret_cast<float*>(base + P.logits) + (size_t)j * T * d.E; };
   auto idx_of = [&](int j) { return reinterpret_cast<int32_t*>(base + P.idx) + (size_t)j * T * d.k; };
@@ -356,9 +341,10 @@ int easybalance_run_pass(const eb_model_desc* desc, int32_t N, int32_t T, float*
         rb.tok0[i + 1] = rb.tok0[i] + T;
         rb.blk0[i + 1] = rb.blk0[i] + (T + 31) / 32;
         rb.e[i] = RouteEntry{x_of(j), gain + (size_t)l * d.H, Wg[l], bias + (size_t)l * d.E, a_of(j),
-                             logits_of(j), idx_of(j), w_of(j), counts_dev + (size_t)j * d.E};
+                             logits_of(j), idx_of(j), w_of(j), counts_dev + (size_t)j * d.E,
+                             balance ? balance + (size_t)l * d.E : nullptr};
       }
-      const hipError_t e = launch_route_batch(d, rb, s);
+      const hipError_t e = launch_route_batch(d, router, rb, s);
       if (e != hipSuccess) return set_error(EB_ERR_HIP, "route launch: %s", hipGetErrorString(e));
     }
     return EB_OK;
@@ -367,7 +353,7 @@ int easybalance_run_pass(const eb_model_desc* desc, int32_t N, int32_t T, float*
   for (int j = 0; j < N; ++j) pool[j] = j;
   if ((rc = route(pool))) return rc;
   if (device)
-    return run_pass_device(d, N, T, P, base, x, gain, Wg, bias, W_gu, W_dn, policy, m, max_steps, n_steps_out,
+    return run_pass_device(d, router, balance, N, T, P, base, x, gain, Wg, bias, W_gu, W_dn, policy, m, max_steps, n_steps_out,
                            runsets_out, layers_out, step_load_out, groups_out, layer_loads_out, placement, s);
   // host-scheduled: the pool's counts come back through this thread's pinned buffer
   int32_t* counts = t_pinned.get((size_t)N * d.E);
@@ -462,6 +448,49 @@ int easybalance_run_pass(const eb_model_desc* desc, int32_t N, int32_t T, float*
   }
   if (n_steps_out) *n_steps_out = n_steps;
   return EB_OK;
+}
+
+}  // namespace
+}  // namespace eb
+
+using namespace eb;
+
+extern "C" {
+
+int easybalance_pass_state_size(const eb_model_desc* desc, int32_t N, int32_t T, size_t* bytes) {
+  if (desc == nullptr || bytes == nullptr) return set_error(EB_ERR_INVALID_ARG, "desc/bytes is NULL");
+  if (N < 1 || N > EB_MAX_POOL || T < 1) return set_error(EB_ERR_INVALID_ARG, "N=%d T=%d out of range", N, T);
+  size_t wsb = 0;
+  std::vector<int32_t> Ts(N, T);
+  const int rc = easybalance_moe_step_workspace_size(desc, N, Ts.data(), &wsb);
+  if (rc) return rc;
+  *bytes = pass_layout(*desc, N, T).total;
+  return EB_OK;
+}
+
+int easybalance_run_pass(const eb_model_desc* desc, int32_t N, int32_t T, float* x,
+                         const float* gain, const void* const* Wg, const float* bias,
+                         const void* const* W_gu, const void* const* W_dn, int32_t policy,
+                         int32_t m, void* state, size_t state_bytes, int32_t max_steps,
+                         int32_t* n_steps_out, uint64_t* runsets_out, int32_t* layers_out,
+                         int64_t* step_load_out, int32_t* groups_out, int32_t* layer_loads_out,
+                         const eb_placement* placement, void* stream) {
+  return run_pass_common(desc, nullptr, N, T, x, gain, Wg, bias, nullptr, W_gu, W_dn, policy, m, state, state_bytes,
+                         max_steps, n_steps_out, runsets_out, layers_out, step_load_out, groups_out, layer_loads_out,
+                         placement, stream);
+}
+
+int easybalance_run_pass_scored(const eb_model_desc* desc, const eb_router* router, int32_t N, int32_t T, float* x,
+                                const float* gain, const void* const* Wg, const float* bias, const float* balance,
+                                const void* const* W_gu, const void* const* W_dn, int32_t policy, int32_t m,
+                                void* state, size_t state_bytes, int32_t max_steps, int32_t* n_steps_out,
+                                uint64_t* runsets_out, int32_t* layers_out, int64_t* step_load_out,
+                                int32_t* groups_out, int32_t* layer_loads_out, const eb_placement* placement,
+                                void* stream) {
+  if (router == nullptr) return set_error(EB_ERR_INVALID_ARG, "router is NULL");
+  return run_pass_common(desc, router, N, T, x, gain, Wg, bias, balance, W_gu, W_dn, policy, m, state, state_bytes,
+                         max_steps, n_steps_out, runsets_out, layers_out, step_load_out, groups_out, layer_loads_out,
+                         placement, stream);
 }
 
 }  // extern "C"

@@ -559,8 +559,9 @@ void permute_impl(RTA a, const eb_model_desc& d, int grid_chunks, int grid_token
   const int bm = gemm_bm(d.dtype);
   const TailRule tail = gemm_tail(d.dtype, d.F);
   const int elem_bytes = d.dtype == EB_DTYPE_BF16 ? 2 : 4;
+  const bool gather = b.a_perm != nullptr;
   if (perm_small(d, pieces, grid_chunks)) {
-    const bool copy = (long long)grid_tokens * (d.k + d.S) * d.H * elem_bytes <= kSmallCopy;
+    const bool copy = gather && (long long)grid_tokens * (d.k + d.S) * d.H * elem_bytes <= kSmallCopy;
     perm_small_impl(a, b, bm, tail, copy ? d.H * elem_bytes : 0, s);
     if (copy) return;
   } else {
@@ -568,7 +569,7 @@ void permute_impl(RTA a, const eb_model_desc& d, int grid_chunks, int grid_token
     perm_scan_impl(a, b.hist, b.chunk_base, b.offsets, b.tiles, bm, tail, b.max_tiles, b.work_ctr, s);
     perm_scatter_impl(a, grid_chunks, b.chunk_base, b.perm, b.inv, s);
   }
-  gather_impl(a, d.H, grid_tokens, elem_bytes, b.inv, b.a_perm, s);
+  if (gather) gather_impl(a, d.H, grid_tokens, elem_bytes, b.inv, b.a_perm, s);
 }
 
 bool scan_fits(int L, int E, int S, int n) {

@@ -602,7 +602,7 @@ __global__ __launch_bounds__(256, KC == 2 ? 8 : 1) void route_token_kernel(RBA r
         red_z[0][tid] = ze;  // read back by this lane only
         if (z != nullptr) z[(size_t)t * E + tid] = ze;
       }
-      topk_group8<1, 8>(tid, E, k, norm_topk, red_z[0], idx + (size_t)t * k, w + (size_t)t * k);
+      if (norm_topk != kLogitsOnly) topk_group8<1, 8>(tid, E, k, norm_topk, red_z[0], idx + (size_t)t * k, w + (size_t)t * k);
     }
   } else {
 #pragma unroll
@@ -619,7 +619,7 @@ __global__ __launch_bounds__(256, KC == 2 ? 8 : 1) void route_token_kernel(RBA r
       if (z != nullptr) z[(size_t)t * E + tid] = ze;
     }
     __syncthreads();
-    if (tid == 0)
+    if (tid == 0 && norm_topk != kLogitsOnly)
       topk_token(E, k, norm_topk, [&](int e) { return red_z[0][e]; }, idx + (size_t)t * k,
                  w + (size_t)t * k);
   }
@@ -761,6 +761,7 @@ __global__ __launch_bounds__(256) void route_mfma_kernel(RBA rba, int H, int E, 
       }
     }
   }
+  if (norm_topk == kLogitsOnly) return;
   __syncthreads();
   // 8 lanes per token
   const int tl = threadIdx.x >> 3, t = t0 + tl;
@@ -950,7 +951,7 @@ __global__ __launch_bounds__(64 * C::WAVES) void route_lds_kernel(RBA rba, int H
       }
     }
   }
-  if constexpr (HALF) return;
+  if (HALF || norm_topk == kLogitsOnly) return;
   if constexpr (OWN)
     for (int e = threadIdx.x; e < E; e += 64 * C::WAVES) hist[e] = 0;
   __syncthreads();
@@ -1070,7 +1071,8 @@ hipError_t route_batch_typed(const eb_model_desc& d, RBA rba, const RouteBatch* 
   // the matrix-core routers count an entry's picks themselves where one
   // workgroup holds the whole entry
   const bool halves = z_stored && d.E > 128 && grid_tokens <= kRouteHalvesTokens;
-  const bool own = !halves && sizeof(TA) == 2 && one_block && !fused_token_path<TA>(d);
+  const bool picks = d.norm_topk != kLogitsOnly;
+  const bool own = picks && !halves && sizeof(TA) == 2 && one_block && !fused_token_path<TA>(d);
   if (grid_tokens > 0) {
     if (fused_token_path<TA>(d)) {
       prof_start(EB_K_ROUTE_LOGITS, s);
@@ -1117,7 +1119,7 @@ hipError_t route_batch_typed(const eb_model_desc& d, RBA rba, const RouteBatch* 
           own ? route_lds_launch<RouteTile32x256, true>(d, rba, grid_blocks, s)
               : route_lds_launch<RouteTile32x256, false>(d, rba, grid_blocks, s);
         prof_stop(EB_K_ROUTE_LOGITS, s);
-        if (halves) {
+        if (halves && picks) {
           prof_start(EB_K_ROUTE_TOPK, s);
           hipLaunchKernelGGL((topk_rows_kernel<8, RBA>), dim3(grid_blocks), dim3(256), 0, s, rba, d.E, d.k, d.norm_topk);
           prof_stop(EB_K_ROUTE_TOPK, s);
@@ -1134,6 +1136,7 @@ hipError_t route_batch_typed(const eb_model_desc& d, RBA rba, const RouteBatch* 
                              static_cast<const TA*>(e.Wg), e.bias, e.z);
         }
         prof_stop(EB_K_ROUTE_LOGITS, s);
+        if (!picks) return hipGetLastError();
         prof_start(EB_K_ROUTE_TOPK, s);
         for (int i = 0; i < rb.n; ++i) {
           const int T = rb.tok0[i + 1] - rb.tok0[i];
@@ -1146,7 +1149,7 @@ hipError_t route_batch_typed(const eb_model_desc& d, RBA rba, const RouteBatch* 
       }
     }
   }
-  if (grid_entries > 0 && !own) {
+  if (grid_entries > 0 && picks && !own) {
     prof_start(EB_K_ROUTE_TOPK, s);
     hipLaunchKernelGGL((counts_kernel<RBA>), dim3(grid_entries), dim3(1024), 0, s, rba, d.k, d.E);
     prof_stop(EB_K_ROUTE_TOPK, s);
@@ -1156,7 +1159,7 @@ hipError_t route_batch_typed(const eb_model_desc& d, RBA rba, const RouteBatch* 
 
 }  // namespace
 
-hipError_t launch_route_batch(const eb_model_desc& d, const RouteBatch& rb, hipStream_t s) {
+static hipError_t route_batch_host(const eb_model_desc& d, const RouteBatch& rb, hipStream_t s) {
   const ByValue<RouteBatch> a{rb};
   bool one = true, z = true;
   for (int i = 0; i < rb.n; ++i) {
@@ -1168,26 +1171,43 @@ hipError_t launch_route_batch(const eb_model_desc& d, const RouteBatch& rb, hipS
   return route_batch_typed<float>(d, a, &rb, rb.n, rb.tok0[rb.n], rb.blk0[rb.n], one, z, s);
 }
 
+// With a router: the norm and the logits, then launch_select_batch's picks.
+hipError_t launch_route_batch(const eb_model_desc& desc, const eb_router* router, const RouteBatch& rb, hipStream_t s) {
+  eb_model_desc d = desc;
+  d.dtype = act_dtype(d.dtype);
+  if (router == nullptr) return route_batch_host(d, rb, s);
+  d.norm_topk = kLogitsOnly;
+  const hipError_t e = route_batch_host(d, rb, s);
+  return e != hipSuccess ? e : launch_select_batch(*router, d.E, d.k, rb, s);
+}
+
 bool route_logits_required(const eb_model_desc& d) {
-  return d.dtype != EB_DTYPE_BF16 && !fused_token_path<float>(d);
+  return act_dtype(d.dtype) != EB_DTYPE_BF16 && !fused_token_path<float>(d);
 }
 
 bool route_batch_device_ok(const eb_model_desc& d) {
-  return d.dtype == EB_DTYPE_BF16 || fused_token_path<float>(d);
+  return act_dtype(d.dtype) == EB_DTYPE_BF16 || fused_token_path<float>(d);
 }
 
-hipError_t launch_route_batch_dev(const eb_model_desc& d, const RouteBatch* rb, int max_entries, int T,
-                                  hipStream_t s) {
-  if (!route_batch_device_ok(d) || max_entries > kRouteBatch) return hipErrorInvalidValue;
+hipError_t launch_route_batch_dev(const eb_model_desc& desc, const eb_router* router, const RouteBatch* rb,
+                                  int max_entries, int T, hipStream_t s) {
+  if (!route_batch_device_ok(desc) || max_entries > kRouteBatch) return hipErrorInvalidValue;
+  eb_model_desc d = desc;
+  d.dtype = act_dtype(d.dtype);
+  if (router) d.norm_topk = kLogitsOnly;
   const InMemory<RouteBatch> a{rb};
   const int tokens = max_entries * T, blocks = max_entries * ((T + 31) / 32);
   const bool one = T >= 1 && T <= 32;
-  if (d.dtype == EB_DTYPE_BF16) return route_batch_typed<bf16_t>(d, a, nullptr, max_entries, tokens, blocks, one, true, s);
-  return route_batch_typed<float>(d, a, nullptr, max_entries, tokens, blocks, one, true, s);
+  const hipError_t e =
+      d.dtype == EB_DTYPE_BF16
+          ? route_batch_typed<bf16_t>(d, a, nullptr, max_entries, tokens, blocks, one, true, s)
+          : route_batch_typed<float>(d, a, nullptr, max_entries, tokens, blocks, one, true, s);
+  if (e != hipSuccess || router == nullptr) return e;
+  return launch_select_batch_dev(*router, d.E, d.k, rb, max_entries, T, s);
 }
 
-hipError_t launch_route(const eb_model_desc& d, int T, const float* x, const float* gain,
-                        const void* Wg, const float* bias, void* a_out, float* logits,
+hipError_t launch_route(const eb_model_desc& d, const eb_router* router, int T, const float* x, const float* gain,
+                        const void* Wg, const float* bias, const float* balance, void* a_out, float* logits,
                         int32_t* idx, float* w, int32_t* counts, hipStream_t s) {
   RouteBatch rb;
   rb.n = 1;
@@ -1195,8 +1215,8 @@ hipError_t launch_route(const eb_model_desc& d, int T, const float* x, const flo
   rb.tok0[1] = T;
   rb.blk0[0] = 0;
   rb.blk0[1] = (T + 31) / 32;
-  rb.e[0] = RouteEntry{x, gain, Wg, bias, a_out, logits, idx, w, counts};
-  return launch_route_batch(d, rb, s);
+  rb.e[0] = RouteEntry{x, gain, Wg, bias, a_out, logits, idx, w, counts, balance};
+  return launch_route_batch(d, router, rb, s);
 }
 
 }  // namespace eb

@@ -421,7 +421,8 @@ __global__ __launch_bounds__(kSchedThreads) void sched_step_kernel(DevPassArgs A
                            A.z + (size_t)j * A.T * E,
                            A.idx + (size_t)j * A.T * A.k,
                            A.w + (size_t)j * A.T * A.k,
-                           A.counts + (size_t)j * E};
+                           A.counts + (size_t)j * E,
+                           A.balance ? A.balance + (size_t)l_new * E : nullptr};
     }
     if (run) st->layer[tid] = l_new;
     int lag = L - l_new;

@@ -1,0 +1,316 @@
+"""8-bit experts on the GPU against the oracle in float64: weight quantisation
+and packing bit for bit, the step within the bound that the oracle derives (see
+experts8.expert_ffn8), the same bits in every schedule."""
+import functools
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import experts8 as o8
+from oracle import permute as operm
+
+pytestmark = pytest.mark.gpu
+F8 = torch.float8_e4m3fn
+
+
+def _binding():
+    from paper_2608_07964_amd import binding as B
+    B.lib()
+    return B
+
+
+def to64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+# ---- weights -----------------------------------------------------------------
+
+@pytest.mark.parametrize("which", ["gate_up", "down"])
+@pytest.mark.parametrize("src", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,H,F", [(1, 256, 128), (3, 512, 384), (2, 256, 8320)])
+def test_quantize_weights(n, H, F, src, which):
+    B = _binding()
+    d = B.make_desc(1, H, F, 4, 1, 0, 1, "fp8")
+    N, K = (2 * F, H) if which == "gate_up" else (H, F)
+    g = torch.Generator(device="cuda").manual_seed(N + K)
+    w = torch.randn(n, N, K, generator=g, device="cuda") * torch.exp(3 * torch.randn(n, N, 1, generator=g, device="cuda"))
+    w[0, :128, :128] = 0                          # a block of zeros
+    w[0, 0, 5] = -0.0
+    if K > 128:
+        w[0, :128, 128:256] *= 1e-38              # subnormal values, the smallest scale
+        w[n - 1, 130, 200] = float("nan")         # in a block of numbers
+        w[n - 1, 140, 201] = float("inf")
+    w[0, 128 % N, 0] = 448 * 2.0 ** 3             # on the border between two scales
+    w = w.to(src)
+    q = torch.full((n, N, K), 0x55, dtype=torch.uint8, device="cuda")
+    s = torch.zeros(n, N // 128, K // 128, device="cuda")
+    B.easybalance_quantize_weights(d, B.EB_WEIGHTS_GATE_UP if which == "gate_up" else B.EB_WEIGHTS_DOWN, n, w, q, s)
+    torch.cuda.synchronize()
+    for i in range(n):
+        qr, sr = o8.quantize_blocks(to64(w[i]))
+        assert np.array_equal(to64(s[i]), sr)
+        assert np.array_equal(to64(q[i].view(F8)), qr, equal_nan=True)
+
+
+def test_pack_weights_fp8():
+    """The documented layout: blocks of 256 rows x 128 bytes, then the scales."""
+    B = _binding()
+    n, H, F = 2, 512, 384
+    d = B.make_desc(1, H, F, 4, 1, 0, 1, "fp8")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for kind, N, K in ((B.EB_WEIGHTS_GATE_UP, 2 * F, H), (B.EB_WEIGHTS_DOWN, H, F)):
+        q = torch.randint(0, 256, (n, N, K), generator=g, device="cuda", dtype=torch.int32).to(torch.uint8)
+        s = torch.rand(n, N // 128, K // 128, generator=g, device="cuda")
+        size = B.easybalance_packed_fp8_size(d, kind, n)
+        dst = torch.zeros(size + 64, dtype=torch.uint8, device="cuda")
+        B.easybalance_pack_weights_fp8(d, kind, n, q, s, dst)
+        out, qn = dst.cpu().numpy(), q.cpu().numpy()
+        assert not out[size:].any()
+        blocks = out[:n * N * K].reshape(n, K // 128, N // 256, 256, 8, 16)
+        r, c = np.arange(256)[:, None], np.arange(8)[None, :]
+        for t in range(N // 256):
+            row = 256 * t + r if kind == B.EB_WEIGHTS_DOWN else \
+                128 * t + 32 * (r // 64) + np.where(r % 64 < 32, r % 64, r % 64 - 32 + F)
+            for st in range(K // 128):
+                col = 128 * st + 16 * (c ^ ((r >> 1) & 7))
+                want = qn[:, row[:, :, None], col[:, :, None] + np.arange(16)]
+                assert np.array_equal(blocks[:, st, t], want)
+        assert np.array_equal(out[n * N * K:size].view(np.float32), s.cpu().numpy().reshape(-1))
+
+
+# ---- the step ----------------------------------------------------------------
+
+class Case:
+    """Weights, micro-batches and buffers of one step."""
+
+    def __init__(self, H, F, E, k, S, L, plan, seed=0, pow2=False, scale=0.05, idx=None, spread=0.0):
+        B = self.B = _binding()
+        self.H, self.F, self.E, self.k, self.S, self.L, self.plan = H, F, E, k, S, L, plan
+        self.desc = B.make_desc(L, H, F, E, k, S, 1, "fp8")
+        rng = self.rng = np.random.default_rng(seed)
+        ES = E + S
+
+        def weights(N, K):
+            q = o8.round_e4m3(np.clip(rng.normal(size=(ES, N, K)) * 120, -448, 448))
+            s = scale / 120 * np.exp(0.5 * rng.normal(size=(ES, N // 128, K // 128)))
+            if pow2:
+                s = 2.0 ** np.round(np.log2(s))
+            return q, s.astype(np.float32).astype(np.float64)
+        self.gu = [weights(2 * F, H) for _ in range(L)]
+        self.dn = [weights(H, F) for _ in range(L)]
+        self.Wgu = [self.pack(B.EB_WEIGHTS_GATE_UP, w) for w in self.gu]
+        self.Wdn = [self.pack(B.EB_WEIGHTS_DOWN, w) for w in self.dn]
+        self.a, self.idx, self.w = [], [], []
+        for i, (l, T) in enumerate(plan):
+            a = rng.normal(size=(max(T, 1), H)) * np.exp(spread * rng.normal(size=(max(T, 1), H)))
+            self.a.append(torch.from_numpy(a.astype(np.float32)).cuda().to(torch.bfloat16))
+            picks = np.stack([rng.permutation(E)[:k] for _ in range(max(T, 1))]) if idx is None else idx[i]
+            self.idx.append(torch.from_numpy(np.ascontiguousarray(picks, np.int32)).cuda())
+            self.w.append(torch.rand(max(T, 1), k, device="cuda"))
+        self.P = sum(T for _, T in plan) * (k + S)
+        self.ws_bytes = B.easybalance_moe_step_workspace_size(self.desc, [T for _, T in plan])
+        self.ws = torch.full((self.ws_bytes + 256,), 0xa5, dtype=torch.uint8, device="cuda")
+        self.wsp = self.ws.data_ptr() + (-self.ws.data_ptr()) % 256
+        self.o = torch.full((self.P + 1, H), -7.0, dtype=torch.bfloat16, device="cuda")
+        self.inv = torch.full((self.P + 1,), -7, dtype=torch.int32, device="cuda")
+
+    def pack(self, kind, w):
+        q, s = w
+        qt = torch.from_numpy(q.astype(np.float32)).cuda().to(F8)
+        st = torch.from_numpy(s.astype(np.float32)).cuda()
+        dst = torch.empty(self.B.easybalance_packed_fp8_size(self.desc, kind, len(q)), dtype=torch.uint8, device="cuda")
+        self.B.easybalance_pack_weights_fp8(self.desc, kind, len(q), qt, st, dst)
+        torch.cuda.synchronize()
+        return dst
+
+    def work(self):
+        return self.B.work_array((i, l, T, a, ix, w) for i, ((l, T), a, ix, w) in
+                                 enumerate(zip(self.plan, self.a, self.idx, self.w)))
+
+    def run(self, views=None, stream=None):
+        self.B.easybalance_moe_step(self.desc, self.work(), len(self.plan), self.Wgu, self.Wdn, self.wsp,
+                                    self.ws_bytes, self.o, self.inv, views, stream)
+        return self
+
+    def step_keys(self):
+        return operm.step_keys([(l, ix.cpu().numpy()[:T]) for (l, T), ix in zip(self.plan, self.idx)], self.E, self.S)
+
+    def check(self):
+        torch.cuda.synchronize()
+        ES, slots = self.E + self.S, self.k + self.S
+        perm, inv, off = operm.stable_permutation(self.step_keys(), self.L * ES)
+        assert np.array_equal(self.inv[:self.P].cpu().numpy(), inv)
+        assert self.inv[self.P] == -7 and (self.o[self.P] == -7).all()
+        a = np.concatenate([to64(a[:T]) for (_, T), a in zip(self.plan, self.a)])
+        o, worst = to64(self.o[:self.P]), 0.0
+        for key in np.nonzero(np.diff(off))[0]:
+            l, e = divmod(int(key), ES)
+            rows = slice(off[key], off[key + 1])
+            ref, tol = o8.expert_ffn8(a[perm[rows] // slots], (self.gu[l][0][e], self.gu[l][1][e]),
+                                      (self.dn[l][0][e], self.dn[l][1][e]))
+            tol = o8.stored_bound(ref, tol)
+            err = np.abs(o[rows] - ref)
+            assert np.isfinite(o[rows]).all()
+            assert (err <= tol + 1e-30).all(), (int(key), float((err / (tol + 1e-30)).max()))
+            worst = max(worst, float((err / (tol + 1e-30)).max()))
+            # the bound is small beside the values themselves (but for rows
+            # with a block whose scale is on the border)
+            assert np.median(tol) <= 0.1 * np.sqrt((ref ** 2).mean())
+        return worst
+
+
+SIZES = [  # H, F, E, k, S, L, plan [(layer, T)]
+    (256, 128, 4, 2, 0, 1, [(0, 1)]),
+    (256, 128, 1, 1, 0, 1, [(0, 33)]),
+    (512, 384, 6, 2, 1, 2, [(0, 40), (1, 7), (0, 0), (1, 25)]),
+    (768, 640, 3, 1, 1, 1, [(0, 70)]),                # 65..128-row tiles, 5 K blocks down
+    (512, 256, 2, 1, 0, 1, [(0, 330)]),               # 129..256 rows
+    (256, 128, 1, 1, 0, 1, [(0, 700)]),               # several row tiles to a group
+    (8448, 128, 2, 1, 0, 1, [(0, 9)]),                # 66 K blocks: two sets of scales
+    (256, 8320, 2, 1, 0, 1, [(0, 140)]),              # 65 K blocks down
+    (1024, 512, 40, 6, 2, 3, [(2, 50), (0, 1), (1, 129)]),
+]
+
+
+@pytest.mark.parametrize("pow2", [False, True], ids=["fp32_scales", "pow2_scales"])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s[:6])) + "_" + "+".join(str(t) for _, t in s[6]))
+def test_step(size, pow2):
+    Case(*size, seed=sum(size[:6]), pow2=pow2).run().check()
+
+
+def test_step_of_outlying_activations():
+    """Magnitudes over a wide range within a row: blocks with scales of their own, e4m3's subnormal values."""
+    Case(512, 384, 4, 2, 0, 1, [(0, 60)], seed=5, spread=2.0).run().check()
+
+
+def test_zero_rows_and_experts_nobody_picks():
+    c = Case(512, 256, 8, 2, 0, 1, [(0, 50)], seed=6, idx=[np.tile([[5, 2]], (50, 1))])
+    c.a[0][10] = 0
+    c.run()
+    torch.cuda.synchronize()
+    c.check()
+    assert (c.o[c.inv[20:22].long()] == 0).all()
+
+
+def test_non_finite_activations_stay_in_their_row():
+    c = Case(512, 256, 4, 2, 0, 1, [(0, 80)], seed=7)
+    clean = c.run().o.clone()
+    c.a[0][3, 17], c.a[0][9, 200], c.a[0][9, 201] = float("nan"), float("inf"), -float("inf")
+    c.run()
+    torch.cuda.synchronize()
+    hit = c.inv[:160].long().reshape(80, 2)[[3, 9]].reshape(-1)
+    assert torch.isnan(c.o[hit].float()).all()
+    rest = torch.ones(160, dtype=torch.bool, device="cuda")
+    rest[hit] = False
+    assert torch.equal(c.o[:160][rest].view(torch.int16), clean[:160][rest].view(torch.int16))
+
+
+def test_empty_step_writes_nothing():
+    c = Case(256, 128, 4, 2, 1, 1, [(0, 0), (0, 0)])
+    c.run()
+    torch.cuda.synchronize()
+    assert (c.o == -7).all() and (c.inv == -7).all()
+
+
+def test_views_and_out_of_range_ids():
+    c = Case(256, 256, 4, 2, 1, 2, [(1, 20), (0, 9)], seed=8)
+    perm = torch.full((c.P,), -1, dtype=torch.int32, device="cuda")
+    off = torch.full((c.L * 5 + 1,), -1, dtype=torch.int32, device="cuda")
+    c.run(views=dict(perm=perm, offsets=off)).check()
+    p, _, o = operm.stable_permutation(c.step_keys(), c.L * 5)
+    assert np.array_equal(perm.cpu().numpy(), p) and np.array_equal(off.cpu().numpy(), o)
+    c.idx[0][3, 0], c.idx[0][4, 1] = -5, 99          # clamped to 0 and 3
+    c.run()
+    got = c.o[:c.P].clone()
+    c.idx[0][3, 0], c.idx[0][4, 1] = 0, 3
+    c.run()
+    torch.cuda.synchronize()
+    if not (c.idx[0][3] == 0).all() and not (c.idx[0][4] == 3).all():
+        assert torch.equal(got.view(torch.int16), c.o[:c.P].view(torch.int16))
+
+
+@pytest.mark.parametrize("T", [4, 60, 300])
+def test_a_token_that_picks_an_expert_twice(T):
+    """Both slots have the same grouped row and the same result; the group's
+    other rows are not read as tokens."""
+    E, k = 6, 3
+    rng = np.random.default_rng(T)
+    picks = np.stack([rng.permutation(E)[:k] for _ in range(T)])
+    picks[1::3, 2] = picks[1::3, 0]
+    c = Case(256, 128, E, k, 0, 1, [(0, T)], seed=9, idx=[picks]).run()
+    torch.cuda.synchronize()
+    inv = c.inv[:c.P].cpu().numpy().reshape(T, k)
+    assert np.array_equal(inv[1::3, 2], inv[1::3, 0])
+    a, o = to64(c.a[0]), to64(c.o)
+    for t in range(T):
+        for r in range(k):
+            e = picks[t, r]
+            ref, tol = o8.expert_ffn8(a[t:t + 1], (c.gu[0][0][e], c.gu[0][1][e]), (c.dn[0][0][e], c.dn[0][1][e]))
+            assert (np.abs(o[inv[t, r]] - ref[0]) <= o8.stored_bound(ref, tol)[0] + 1e-30).all()
+
+
+def test_rows_do_not_depend_on_the_step():
+    """A micro-batch alone, and with others around it: the same bits."""
+    big = Case(512, 384, 5, 2, 1, 2, [(0, 300), (1, 45), (0, 130)], seed=10).run()
+    torch.cuda.synchronize()
+    slots, at = 3, [0, 300, 345]
+    for i, (l, T) in enumerate(big.plan):
+        for rows in ([T], [T // 3]):
+            n = rows[0]
+            one = Case.__new__(Case)
+            one.__dict__.update(big.__dict__)
+            one.plan, one.P = [(l, n)], n * slots
+            one.a, one.idx, one.w = [big.a[i][:n].clone()], [big.idx[i][:n].clone()], [big.w[i][:n].clone()]
+            one.o, one.inv = torch.empty_like(big.o), torch.empty_like(big.inv)
+            one.run()
+            torch.cuda.synchronize()
+            q = torch.arange(n * slots, device="cuda")
+            x, y = one.o[one.inv[q].long()], big.o[big.inv[at[i] * slots + q].long()]
+            assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
+def test_two_calls_on_two_streams_and_a_graph():
+    a, b = (Case(512, 256, 8, 2, 1, 2, [(0, 50), (1, 77)], seed=s) for s in (11, 12))
+    want = []
+    for c in (a, b):
+        c.run().check()
+        want.append(c.o.clone())
+        c.o.fill_(-7)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(4):
+        for c, s in zip((a, b), streams):
+            c.run(stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for c, w in zip((a, b), want):
+        assert torch.equal(c.o.view(torch.int16), w.view(torch.int16))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.run(stream=torch.cuda.current_stream().cuda_stream)
+    kept = [t.clone() for t in a.a]
+    for i in range(4):
+        for t, x in zip(a.a, kept):
+            t.copy_(x if i % 2 == 0 else -x)
+        a.o.fill_(-7)
+        a.ws.fill_(0x5a + i)  # nothing in it is kept from one call to the next
+        graph.replay()
+        torch.cuda.synchronize()
+        got = a.o.clone()
+        a.run()
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.int16), a.o.view(torch.int16))
+
+
+def test_quantised_weights_through_a_step():
+    """Weights from bf16 by easybalance_quantize_weights, packed and run."""
+    c = Case(512, 384, 4, 2, 1, 1, [(0, 90)], seed=13)
+    B, g = c.B, torch.Generator(device="cuda").manual_seed(13)
+    for kind, N, K, packed, ref in ((B.EB_WEIGHTS_GATE_UP, 768, 512, c.Wgu, c.gu), (B.EB_WEIGHTS_DOWN, 512, 384, c.Wdn, c.dn)):
+        w = (torch.randn(5, N, K, generator=g, device="cuda") * 0.03).to(torch.bfloat16)
+        q, s = torch.empty(5, N, K, dtype=F8, device="cuda"), torch.empty(5, N // 128, K // 128, device="cuda")
+        B.easybalance_quantize_weights(c.desc, kind, 5, w, q, s)
+        B.easybalance_pack_weights_fp8(c.desc, kind, 5, q, s, packed[0])
+        torch.cuda.synchronize()
+        ref[0] = (to64(q), to64(s))
+    c.run().check()

@@ -1,0 +1,204 @@
+"""Scored routing on the GPU against the oracle in float64: idx and counts are
+equal, w within the bound below, whatever the mask, the ties and the sizes."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import experts8 as o8
+
+pytestmark = pytest.mark.gpu
+
+# fp32 scores: 2^-22 relative for a sigmoid, 38 roundings and the exponential's
+# (d 2^-24 for a distance d < 90 to the largest logit, twice) for a softmax,
+# then the sum of the picks, the quotient and the scale: below 2^-16
+W_REL = 2.0 ** -16
+
+
+def _binding():
+    from paper_2608_07964_amd import binding as B
+    B.lib()
+    return B
+
+
+def run_select(z, k, *, balance=None, stream=None, **kw):
+    B = _binding()
+    T, E = z.shape
+    zt = torch.from_numpy(np.ascontiguousarray(z, np.float32)).cuda()
+    bt = None if balance is None else torch.from_numpy(np.asarray(balance, np.float32)).cuda()
+    idx = torch.full((T + 1, k), -7, dtype=torch.int32, device="cuda")
+    w = torch.full((T + 1, k), -7.0, device="cuda")
+    counts = torch.full((E + 1,), 99, dtype=torch.int32, device="cuda")
+    B.easybalance_select(T, E, k, B.make_router(**kw), zt, bt, idx, w, counts, stream)
+    torch.cuda.synchronize()
+    assert (idx[T] == -7).all() and (w[T] == -7).all() and counts[E] == 99  # nothing past the end
+    return idx[:T].cpu().numpy(), w[:T].cpu().numpy().astype(np.float64), counts[:E].cpu().numpy()
+
+
+def check(z, k, *, balance=None, **kw):
+    z = np.asarray(z, np.float32)
+    b = None if balance is None else np.asarray(balance, np.float32)
+    got, want = run_select(z, k, balance=b, **kw), o8.select(z, k, balance=b, **kw)
+    bad = np.nonzero((got[0] != want[0]).any(axis=1))[0]
+    assert not len(bad), (bad[:5], got[0][bad[:2]], want[0][bad[:2]])
+    assert np.array_equal(got[2], want[2])
+    assert np.array_equal(np.isnan(got[1]), np.isnan(want[1]))
+    ok = np.isfinite(want[1])
+    assert np.array_equal(got[1][~ok & ~np.isnan(want[1])], want[1][~ok & ~np.isnan(want[1])])
+    err = np.abs(got[1] - want[1])[ok]
+    assert (err <= W_REL * np.abs(want[1][ok]) + 1e-37).all(), err.max()
+
+
+# E, k, n_group, topk_group, group_top: whole and partial teams, every lane
+# count per group, one to 31 experts in a lane
+SHAPES = [(256, 8, 8, 4, 2), (160, 6, 8, 3, 1), (60, 4, 1, 1, 2), (64, 6, 1, 1, 2), (1, 1, 1, 1, 1), (2, 2, 2, 2, 1),
+          (3, 2, 1, 1, 2), (96, 8, 32, 5, 2), (255, 8, 5, 2, 2), (128, 16, 64, 9, 2), (64, 1, 64, 1, 1),
+          (1024, 16, 1, 1, 2), (1023, 3, 33, 2, 2), (1000, 16, 40, 3, 1), (1024, 16, 64, 64, 2), (17, 16, 1, 1, 2),
+          (272, 8, 17, 4, 2), (500, 7, 5, 2, 2)]
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_shapes(shape, score):
+    E, k, G, TG, top = shape
+    rng = np.random.default_rng(E * 100 + k)
+    for T, bal, norm, scale in ((1, True, 1, 2.5), (33, False, 0, 1.0), (75, True, 1, 16.0)):
+        check(rng.normal(size=(T, E)) * 2, k, balance=rng.normal(size=E) * 0.1 if bal else None, score=score,
+              n_group=G, topk_group=TG, group_top=top, norm_topk=norm, scale=scale)
+
+
+@pytest.mark.parametrize("T", [0, 1, 31, 32, 33, 64, 257, 1000])
+def test_token_counts(T):
+    rng = np.random.default_rng(T)
+    check(rng.normal(size=(T, 256)), 8, balance=rng.normal(size=256) * 0.05, score="sigmoid", n_group=8, topk_group=4)
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_ties_go_to_the_lower_id(score):
+    rng = np.random.default_rng(5)
+    kw = dict(score=score, n_group=8, topk_group=3, group_top=2)
+    check(np.zeros((40, 64)), 6, **kw)                                   # all equal
+    check(rng.integers(-2, 3, size=(300, 64)), 6, **kw)                  # many equal
+    check(rng.integers(-1, 2, size=(100, 64)), 6, balance=rng.integers(0, 2, 64) * 0.5, **kw)
+    z = rng.integers(0, 2, size=(50, 64)).astype(np.float32)             # neighbours one fp32 step apart
+    check(np.where(z > 0, np.nextafter(np.float32(1), np.float32(2)), np.float32(1)), 6, **kw)
+    check(np.where(z > 0, -0.0, 0.0), 6, **kw)
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_close_scores_are_decided_exactly(score):
+    """Scores a few fp32 steps apart, told apart by the logits or the balance only."""
+    rng = np.random.default_rng(6)
+    z = 0.3 + rng.integers(-40, 40, size=(400, 128)) * 2.0 ** -23
+    check(z, 8, score=score, n_group=8, topk_group=4)
+    b = rng.integers(-3, 4, size=128) * 2.0 ** -22
+    check(z, 8, balance=b, score=score, n_group=8, topk_group=4)
+    check(12 + 4 * rng.random((200, 128)), 8, score=score)  # sigmoids at 1 - 2^-17 and above
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_masks_infinities_and_nan(score):
+    rng = np.random.default_rng(7)
+    kw = dict(score=score, n_group=4, topk_group=2, group_top=2)
+    z = rng.normal(size=(64, 32))
+    z[rng.random(z.shape) < 0.5] = -np.inf
+    z[3] = -np.inf                      # a row that the mask leaves empty
+    z[4, 1:] = -np.inf
+    z[5] = -200 + rng.normal(size=32)   # scores that fp32 does not hold
+    z[6] = -3e38
+    z[7] = np.finfo(np.float32).min
+    z[8, 5] = np.nan
+    z[9] = np.nan
+    z[10, ::2] = np.nan
+    z[11, 4] = np.inf
+    z[12, 4:6] = np.inf
+    for norm in (0, 1):
+        check(z, 6, norm_topk=norm, **kw)
+        check(z, 6, balance=rng.normal(size=32) * 0.1, norm_topk=norm, **kw)
+    bal = np.zeros(32)
+    bal[rng.permutation(32)[:27]] = -np.inf  # fewer experts than picks
+    check(rng.normal(size=(40, 32)), 6, balance=bal, **kw)
+    bal[bal < 0] = -1e9
+    check(rng.normal(size=(40, 32)), 6, balance=bal, **kw)
+    bal[:] = np.finfo(np.float32).min
+    check(rng.normal(size=(40, 32)), 6, balance=bal, **kw)
+    bal[3] = np.nan
+    bal[4] = np.inf
+    check(rng.normal(size=(40, 32)), 6, balance=bal, **kw)
+
+
+def test_large_launch_and_repeat_is_the_same_bits():
+    rng = np.random.default_rng(8)
+    z = rng.normal(size=(6000, 256)).astype(np.float32)
+    kw = dict(balance=rng.normal(size=256) * 0.05, score="sigmoid", n_group=8, topk_group=4, scale=2.5)
+    a, b = run_select(z, 8, **kw), run_select(z, 8, **kw)
+    assert all(np.array_equal(x, y) for x, y in zip(a, b))
+    # a token's row does not depend on the others
+    c = run_select(z[4000:4021], 8, **kw)
+    assert np.array_equal(a[0][4000:4021], c[0]) and np.array_equal(a[1][4000:4021], c[1])
+    want = o8.select(z[:700], 8, **kw)
+    assert np.array_equal(a[0][:700], want[0])
+
+
+@pytest.mark.parametrize("dtype,H,E,k,T", [("bf16", 512, 64, 6, 70), ("bf16", 512, 8, 2, 33), ("bf16", 512, 256, 8, 40),
+                                           ("bf16", 512, 256, 8, 5000), ("bf16", 512, 100, 6, 20), ("bf16", 512, 64, 6, 20),
+                                           ("f32", 512, 40, 4, 50), ("f32", 512, 96, 4, 50), ("f32", 256, 8, 2, 9),
+                                           ("fp8", 512, 64, 6, 70), ("fp8", 256, 16, 4, 0)])
+def test_route_scored(dtype, H, E, k, T):
+    """a and the logits of easybalance_route bit for bit, and the picks that
+    easybalance_select takes from them."""
+    B = _binding()
+    g = torch.Generator(device="cuda").manual_seed(E + T)
+    tdt = torch.float32 if dtype == "f32" else torch.bfloat16
+    x = torch.randn(max(T, 1), H, generator=g, device="cuda")
+    gain = 1 + 0.1 * torch.randn(H, generator=g, device="cuda")
+    Wg = (torch.randn(E, H, generator=g, device="cuda") * H ** -0.5).to(tdt)
+    bias, bal = (0.2 * torch.randn(E, generator=g, device="cuda") for _ in range(2))
+    d = B.make_desc(1, H, 128, E, k, 0, 1, dtype)
+    G = next(n for n in (8, 5, 4, 2) if E % n == 0)
+    kw = dict(score="sigmoid", n_group=G, topk_group=(G + 1) // 2, group_top=1, scale=2.5)
+
+    def outputs():
+        return dict(a=torch.zeros(max(T, 1), H, dtype=tdt, device="cuda"), z=torch.zeros(max(T, 1), E, device="cuda"),
+                    idx=torch.zeros(max(T, 1), k, dtype=torch.int32, device="cuda"), w=torch.zeros(max(T, 1), k, device="cuda"),
+                    counts=torch.full((E,), 5, dtype=torch.int32, device="cuda"))
+    p, q = outputs(), outputs()
+    B.easybalance_route(d, 0, T, x, gain, Wg, bias, *p.values())
+    B.easybalance_route_scored(d, B.make_router(**kw), 0, T, x, gain, Wg, bias, bal, *q.values())
+    torch.cuda.synchronize()
+    assert torch.equal(p["a"], q["a"]) and torch.equal(p["z"], q["z"])
+    rows = min(T, 200)
+    z = q["z"][:T].cpu().numpy()
+    idx, w, cnt = run_select(z, k, balance=bal.cpu().numpy(), **kw) if T else (None, None, np.zeros(E, np.int32))
+    assert np.array_equal(q["counts"].cpu().numpy(), cnt)
+    if T:
+        assert np.array_equal(q["idx"].cpu().numpy(), idx) and np.array_equal(q["w"].cpu().numpy().astype(np.float64), w)
+        want = o8.select(z[:rows], k, balance=bal.cpu().numpy(), **kw)
+        assert np.array_equal(idx[:rows], want[0])
+
+
+def test_two_streams_and_a_graph():
+    B = _binding()
+    rng = np.random.default_rng(9)
+    zs = [torch.from_numpy(rng.normal(size=(500, 128)).astype(np.float32)).cuda() for _ in range(2)]
+    r = B.make_router("sigmoid", n_group=8, topk_group=4)
+    outs = [(torch.zeros(500, 8, dtype=torch.int32, device="cuda"), torch.zeros(500, 8, device="cuda"),
+             torch.zeros(128, dtype=torch.int32, device="cuda")) for _ in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for z, o, s in zip(zs, outs, streams):
+            B.easybalance_select(500, 128, 8, r, z, None, *o, s.cuda_stream)
+    torch.cuda.synchronize()
+    want = [o8.select(z.cpu().numpy(), 8, score="sigmoid", n_group=8, topk_group=4) for z in zs]
+    for o, w in zip(outs, want):
+        assert np.array_equal(o[0].cpu().numpy(), w[0]) and np.array_equal(o[2].cpu().numpy(), w[2])
+    graph, z, o = torch.cuda.CUDAGraph(), zs[0].clone(), outs[0]
+    with torch.cuda.graph(graph):
+        B.easybalance_select(500, 128, 8, r, z, None, *o, torch.cuda.current_stream().cuda_stream)
+    for i in (1, 0, 1, 0):
+        z.copy_(zs[i])
+        for t in o:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(o[0].cpu().numpy(), want[i][0]) and np.array_equal(o[2].cpu().numpy(), want[i][2])

@@ -57,48 +57,56 @@ def dequantize_blocks(q: np.ndarray, s: np.ndarray) -> np.ndarray:
     return np.asarray(q, np.float64) * np.kron(np.asarray(s, np.float64), np.ones((BLK, BLK)))
 
 
-def expert_ffn8(a: np.ndarray, gu, dn):
-    """o [R][H] before its bf16 rounding, and how far a kernel's fp32 sums may
-    move it, for rows a [R][H] (bf16 values) of one expert; gu, dn: (q, s).
+U = 2.0 ** -24                # half a step of fp32, relative
 
-    The bound counts u = 2^-24 per rounding:
-      y: K products, their sum, and two roundings a block for the scales:
-         (K + 2 K/128) u sum |a w|;
-      h: |silu'| < 1.1, so 1.1 |up| err(gate) + |silu(gate)| err(up), and 8 u |h|
-         for the exponential, the reciprocal and three products;
-      an h within that error of the middle between two e4m3 values may go to
-      the other one, a step away, and a block whose largest |h| is within it of
-      448 times a power of two may take the other scale, with steps twice as
-      large, where every h of the block may be 1.5 steps off: the sum over such
-      h of that times |w|;
-      o: the same as y over F.
-    """
-    u = 2.0 ** -24
-    F, H = gu[0].shape[0] // 2, gu[0].shape[1]
-    aq, sa = quantize_rows(a)
-    ad = aq * np.repeat(sa, BLK, axis=1)
-    w, d = dequantize_blocks(*gu), dequantize_blocks(*dn)
-    y, ay = ad @ w.T, (H + 2 * H / BLK) * u * (np.abs(ad) @ np.abs(w).T)
-    g, up = y[:, :F], y[:, F:]
+
+def product_bound(x: np.ndarray, y: np.ndarray) -> np.ndarray:
+    """How far a kernel's x @ y.T may be off for rows x [R][K], y [N][K] of
+    e4m3 values times their blocks' scales (both scales constant over 128
+    columns): the matrix instruction drops from each of 8 products less than
+    2^-13 of the largest one's power of two (7 of them, the largest loses
+    nothing); the K/8 sums of 8, and two roundings for a scale of each of the
+    K/128 blocks, are fp32."""
+    K = x.shape[1]
+    ax, ay = np.abs(x), np.abs(y)
+    drop = np.zeros((x.shape[0], y.shape[0]))
+    for k in range(0, K, 8):
+        drop += (ax[:, None, k:k + 8] * ay[None, :, k:k + 8]).max(axis=2)
+    return 7 * 2.0 ** -13 * drop + (K / 8 + 2 * K / BLK + 8) * U * (ax @ ay.T)
+
+
+def hidden8(a: np.ndarray, gu):
+    """h [R][F] before it is quantised, in float64, for rows a [R][H] (bf16
+    values) of one expert, and how far a kernel's fp32 h may be off: |silu'| <
+    1.1, so 1.1 |up| err(gate) + |silu(gate)| err(up) (+ their product), and 8 U
+    |h| for the exponential, the reciprocal and three products."""
+    F = gu[0].shape[0] // 2
+    q, s = quantize_rows(a)
+    x, w = q * np.repeat(s, BLK, axis=1), dequantize_blocks(*gu)
+    y, e = x @ w.T, product_bound(x, w)
+    g, up, eg, eu = y[:, :F], y[:, F:], e[:, :F], e[:, F:]
     h = silu(g) * up
-    eh = 1.1 * np.abs(up) * ay[:, :F] + np.abs(silu(g)) * ay[:, F:] + 8 * u * np.abs(h)
-    b, eb = h.reshape(len(h), -1, BLK), eh.reshape(len(h), -1, BLK)
-    amax = np.abs(b).max(axis=2)
-    s = block_scale(amax)
-    q = round_e4m3(b / s[:, :, None])
-    # the two scales a block can have, and whether its other one can come about
-    worst = eb.max(axis=2)
-    other = (block_scale(amax + worst) != s) | (block_scale(np.maximum(amax - worst, 0)) != s)
-    _, e = np.frexp(b / s[:, :, None])
-    step = np.ldexp(1.0, np.maximum(e - 1, -6) - 3) * s[:, :, None]
-    near = np.abs(np.abs(b - q * s[:, :, None]) - step / 2) <= eb
-    # the neighbour across the middle is one step away; under the other scale a
-    # value is rounded by at most half of twice the step instead of half a step
-    slack = np.where(other[:, :, None], 1.5 * step, np.where(near, step, 0.0)).reshape(h.shape)
-    hd = (q * s[:, :, None]).reshape(h.shape)
-    o = hd @ d.T
-    tol = (F + 2 * F / BLK) * u * (np.abs(hd) @ np.abs(d).T) + slack @ np.abs(d).T
-    return o, tol
+    return h, 1.1 * np.abs(up) * eg + (np.abs(silu(g)) + 1.1 * eg) * eu + 8 * U * np.abs(h)
+
+
+def quantised_bound(h: np.ndarray, eh: np.ndarray, s: np.ndarray):
+    """For a kernel's quantised h with scales s [R][F/128], given h and the bound
+    eh on its fp32 values: whether each scale is the one of some |h| within the
+    bound, and how far the e4m3 values times s may be off h (half a step of the
+    larger magnitude, and eh)."""
+    b, e = np.abs(h).reshape(len(h), -1, BLK), eh.reshape(len(h), -1, BLK)
+    lo, hi = block_scale(np.maximum(b - e, 0).max(axis=2)), block_scale((b + e).max(axis=2))
+    ok = (s >= lo) & (s <= hi) | (lo == 1) & (s <= hi)  # all of it may be 0
+    _, x = np.frexp((b + e) / s[:, :, None])
+    half = np.ldexp(1.0, np.maximum(x - 1, -6) - 4) * s[:, :, None]
+    return ok, eh + half.reshape(h.shape)
+
+
+def stored_bound(o: np.ndarray, tol: np.ndarray) -> np.ndarray:
+    """How far a kernel's stored bf16 output may be from o itself: it computes
+    some o' with |o' - o| <= tol and stores bf16(o'), off by at most half a step,
+    2^-8 |o'| <= 2^-8 (|o| + tol)."""
+    return tol + 2.0 ** -8 * (np.abs(o) + tol)
 
 
 def select(z, k: int, *, score: str, balance=None, n_group: int = 1, topk_group: int = 1, group_top: int = 2,
@@ -133,11 +141,3 @@ def select(z, k: int, *, score: str, balance=None, n_group: int = 1, topk_group:
             p = s[idx[t]]
             w[t] = scale * (p / p.sum() if norm_topk and p.sum() != 0 else p)
     return idx, w, np.bincount(idx.reshape(-1), minlength=E).astype(np.int32)
-
-
-def stored_bound(o: np.ndarray, tol: np.ndarray) -> np.ndarray:
-    """How far a kernel's stored output may be from o itself: it computes some
-    o' with |o' - o| <= tol and stores bf16(o'), off by at most half a step,
-    2^-8 |o'| <= 2^-8 (|o| + tol).  (From bf16(o), which is off o by another
-    half step, it may be 2^-8 |o| further.)"""
-    return tol + 2.0 ** -8 * (np.abs(o) + tol)

@@ -72,7 +72,7 @@ StepShape step_shape(const eb_model_desc& d, int n_run, const int32_t* T) {
 
 struct WsLayout {
   size_t hist, chunk_base, offsets, tiles, work_ctr, partial, a_perm, h;
-  size_t perm, qa, sa, sh;  // 8-bit stacks
+  size_t perm, qa, sa;      // 8-bit stacks (their h is followed by its exponents)
   size_t total;
 };
 
@@ -98,8 +98,7 @@ WsLayout ws_layout(const eb_model_desc& d, const StepShape& s, const eb_step_vie
     w.perm = (v && v->perm) ? 0 : take(sizeof(int32_t) * (size_t)s.P);
     w.qa = take((size_t)s.tokens * d.H);
     w.sa = take(exponent_bytes(s.tokens, d.H));
-    w.h = take((size_t)s.P * d.F);
-    w.sh = take(exponent_bytes(s.P, d.F));
+    w.h = (v && v->h) ? 0 : take((size_t)s.P * d.F + exponent_bytes(s.P, d.F));
     w.total = off;
     return w;
   }
@@ -224,8 +223,8 @@ StepWs carve_step(const eb_model_desc& d, const StepShape& sh, const eb_step_vie
     w.partial = nullptr;
     w.qa = base + L.qa;
     w.sa = base + L.sa;
-    w.h = base + L.h;
-    w.sh = base + L.sh;
+    w.h = (views && views->h) ? views->h : base + L.h;
+    w.sh = static_cast<uint8_t*>(w.h) + (size_t)sh.P * d.F;
     return w;
   }
   b.a_perm = (views && views->a_perm) ? views->a_perm : base + L.a_perm;
@@ -503,8 +502,9 @@ int moe_step_common(const eb_model_desc* desc, int32_t n_run, const eb_work* run
   if (d.dtype == EB_DTYPE_FP8) {
     if (static_scratch)
       return set_error(EB_ERR_UNSUPPORTED, "8-bit stacks have no static scratch: use easybalance_moe_step, which allocates nothing either");
-    if (views && (views->a_perm || views->h))
-      return set_error(EB_ERR_UNSUPPORTED, "8-bit stacks have no a_perm and h views");
+    if (views && views->a_perm) return set_error(EB_ERR_UNSUPPORTED, "8-bit stacks gather no rows: no a_perm view");
+    if (views && reinterpret_cast<uintptr_t>(views->h) % 16 != 0)
+      return set_error(EB_ERR_INVALID_ARG, "views->h not 16-byte aligned");
   }
   if (W_gu == nullptr || W_dn == nullptr) return set_error(EB_ERR_INVALID_ARG, "W_gu/W_dn is NULL");
   WeightTable wt;

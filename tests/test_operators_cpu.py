@@ -143,8 +143,10 @@ def test_step_refusals():
     W = [ADDR] * 2
     step = B.easybalance_moe_step
     refused(B.EB_ERR_WORKSPACE_TOO_SMALL, step, d, run, 1, W, W, ADDR, n - 1, ADDR, ADDR)
-    for view in ("a_perm", "h"):
-        refused(NO, step, d, run, 1, W, W, ADDR, n, ADDR, ADDR, {view: ADDR})
+    refused(NO, step, d, run, 1, W, W, ADDR, n, ADDR, ADDR, dict(a_perm=ADDR))
+    refused(BAD, step, d, run, 1, W, W, ADDR, n, ADDR, ADDR, dict(h=ADDR + 8))
+    refused(NO, B.easybalance_moe_step_noalloc, d, run, 1, W, W, ADDR, ADDR, dict(a_perm=ADDR, h=ADDR)) \
+        if torch.cuda.is_available() else None  # takes its scratch's address first
     refused(BAD, step, d, run, 1, [None] * 2, W, ADDR, n, ADDR, ADDR)
     refused(BAD, step, d, run, 1, W, W, ADDR, n, None, ADDR)
     # 2^22 tokens of 512 bytes, and a step whose exponents pass 2^31 bytes

@@ -20,10 +20,12 @@
 // again from fp64 scores.  About 1 token in 100 of 256 experts takes that path.
 //
 // A team of W lanes takes a token.  Its lanes are dealt to the groups (a power
-// of two each), so a lane holds V experts of one group: e = group M + j + i LPG
-// for lane j of the group's LPG lanes, and a group's two largest are a
-// reduction over LPG lanes.  A pick is one maximum of unsigned order keys over
-// the lane's V values and the team, then the lowest id that has it.
+// of two each), so a lane holds up to V consecutive experts of one group: lane j
+// of the group's LPG lanes those from group M + j V on, and a group's two
+// largest are a reduction over LPG lanes.  A pick is one maximum over the lane's
+// values and the team.  The fp32 choice needs no order among equal values (they
+// are close, so fp64 decides) and takes the values as they are; the fp64 choice
+// has a wavefront to itself and goes by unsigned order keys.
 #include "eb_internal.h"
 #include "eb_numeric.h"
 
@@ -40,36 +42,37 @@ constexpr float kMarginSigmoid = 0x1p-21f, kMarginSoftmax = 0x1p-17f;
 // its smallest numbers have few digits).
 constexpr float kTiny = 1e-30f;
 
-// Order-preserving unsigned keys: NaN 1, then -inf .. inf; 0 is no value.
-__device__ __forceinline__ uint32_t order_key(float v) {
-  if (!(v == v)) return 1u;
-  const uint32_t u = __float_as_uint(v == 0.f ? 0.f : v);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
+// Order-preserving unsigned key: NaN 1, then -inf .. inf; 0 is no value.
 __device__ __forceinline__ uint64_t order_key(double v) {
   if (!(v == v)) return 1ull;
   const uint64_t u = (uint64_t)__double_as_longlong(v == 0.0 ? 0.0 : v);
   return (u >> 63) ? ~u : (u | (1ull << 63));
 }
-__device__ __forceinline__ float key_float(uint32_t o) {
-  return o <= 1u ? __builtin_nanf("") : __uint_as_float((o & 0x80000000u) ? (o ^ 0x80000000u) : ~o);
-}
 
-// Value of the lane `off` away by XOR, off a power of two below W: within 16
-// lanes by DPP (for off 4 and 8 a mirror, which serves a reduction whose
-// values are already equal within groups of off lanes).
+// Exchange of a reduction whose values are already equal within groups of OFF
+// lanes: each lane gets the value of the neighbouring group.  Within 16 lanes by
+// DPP (4 and 8 as mirrors), beyond by the swaps of rows and halves.
 template <int OFF>
 __device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
   if constexpr (OFF == 1) return __builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true);
   else if constexpr (OFF == 2) return __builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true);
   else if constexpr (OFF == 4) return __builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true);
   else if constexpr (OFF == 8) return __builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true);
-  else return __shfl_xor((int)v, OFF, 64);
+  else if constexpr (OFF == 16) {
+    // [0] rows 0 0 2 2, [1] rows 1 1 3 3 of v
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return (threadIdx.x & 16) ? r[0] : r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (threadIdx.x & 32) ? r[0] : r[1];
+  }
 }
 template <int OFF>
 __device__ __forceinline__ uint64_t lane_xor(uint64_t v) {
   return ((uint64_t)lane_xor<OFF>((uint32_t)(v >> 32)) << 32) | lane_xor<OFF>((uint32_t)v);
 }
+template <int OFF>
+__device__ __forceinline__ int lane_xor(int v) { return (int)lane_xor<OFF>((uint32_t)v); }
 template <int OFF>
 __device__ __forceinline__ float lane_xor(float v) { return __uint_as_float(lane_xor<OFF>(__float_as_uint(v))); }
 template <int OFF>
@@ -97,184 +100,317 @@ __device__ __forceinline__ double sigmoid_of(double z) { return 1.0 / (1.0 + exp
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 __device__ __forceinline__ double exp_of(double x) { return exp(x); }
 
-// What the lanes of a team hold: lane `sub`'s experts are first + i step for
-// i < V, those below `end` (the end of its group).
+// What a lane of a team holds: experts first + i for i < V, those below end (the
+// end of its group).  Lanes past the last group hold none.
 struct TeamMap {
   int sub, lpg, group, first, end;
 };
+template <int W, int V>
+__device__ __forceinline__ TeamMap team_map(const eb_router& p, int E, int sub) {
+  TeamMap m;
+  m.sub = sub;
+  m.lpg = W;
+  while (m.lpg * p.n_group > W) m.lpg >>= 1;
+  m.group = sub / m.lpg;
+  const int M = E / p.n_group;
+  m.first = m.group * M + (sub % m.lpg) * V;
+  m.end = m.group < p.n_group ? (m.group + 1) * M : 0;
+  return m;
+}
 
 __device__ __forceinline__ float magnitude(float v) { return fabsf(v); }
 __device__ __forceinline__ double magnitude(double v) { return fabs(v); }
 
-// The k picks of one token in type R (float or double): lane r < k returns pick
-// r's expert in *pick and its routing weight in *w.  close: a decision was
-// within the error bound of float, or the picks' sum where fp32 loses digits.
-template <int W, int V, class R>
-__device__ __forceinline__ void choose(const eb_router& p, const TeamMap& m, int E, int k, const float* __restrict__ z,
-                                       const float* __restrict__ balance, int* pick, float* w, bool* close) {
-  using Key = decltype(order_key(R(0)));
-  const auto maxk = [](Key a, Key b) { return a > b ? a : b; };
-  const auto maxr = [](R a, R b) { return a > b ? a : b; };
-  const R ninf = -(R)INFINITY;
-  // softmax: the row's largest logit and denominator.  A row of -inf alone has
-  // s = 0; NaN and +inf logits make every s of the row NaN.
-  R mx = ninf, denom = 1, top = 1;
-  const bool soft = p.score == EB_SCORE_SOFTMAX;
-  R c[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = m.first + i * m.lpg;
-    c[i] = e < m.end ? (R)z[e] : ninf;
+// The row's scores.  softmax: over the row's largest logit and denominator; a
+// row of -inf alone has s = 0, NaN and +inf logits make every s of the row NaN.
+template <bool SOFT, class R>
+struct Scores {
+  R mx, inv;  // inv: 1 / denominator, 0 for a row of -inf alone
+  __device__ __forceinline__ R of(R z) const {
+    if constexpr (!SOFT) return sigmoid_of(z);
+    return exp_of(z - mx) * inv;
   }
-  if (soft) {
+  // an upper bound of the row's scores
+  __device__ __forceinline__ R top() const { return SOFT ? inv : (R)1; }
+};
+template <bool SOFT, int W, int V, class R>
+__device__ __forceinline__ Scores<SOFT, R> row_scores(const R (&z)[V]) {
+  Scores<SOFT, R> s{0, 1};
+  if constexpr (SOFT) {
+    const auto maxr = [](R a, R b) { return a > b ? a : b; };
     bool nan = false;
+    R mx = -(R)INFINITY, sum = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      mx = maxr(mx, c[i]);
-      nan |= !(c[i] == c[i]);
+      mx = maxr(mx, z[i]);
+      nan |= !(z[i] == z[i]);
     }
     mx = team_reduce<W>(mx, maxr);
-    denom = 0;
+    s.mx = mx == -(R)INFINITY ? (R)0 : mx;  // e^(-inf - 0) = 0
 #pragma unroll
-    for (int i = 0; i < V; ++i) denom += mx == ninf ? (R)0 : exp_of(c[i] - mx);
-    if (nan) denom = (R)__builtin_nan("");
-    denom = team_reduce<W>(denom, [](R a, R b) { return a + b; });
-    if (denom == 0) denom = 1;  // a row of -inf alone
-    top = 1 / denom;
+    for (int i = 0; i < V; ++i) sum += exp_of(z[i] - s.mx);
+    if (nan) sum = (R)__builtin_nan("");
+    sum = team_reduce<W>(sum, [](R a, R b) { return a + b; });
+    s.inv = sum == 0 ? (R)0 : 1 / sum;
   }
-  auto score = [&](R v) -> R {
-    if (!soft) return sigmoid_of(v);
-    return (mx == ninf ? (R)0 : exp_of(v - mx)) / denom;
-  };
+  return s;
+}
+
+// The lane's V values of a row (none: past its end); vec: in 16-byte loads.
+template <int V>
+__device__ __forceinline__ void load_lane(float (&c)[V], const TeamMap& m, bool vec, const float* __restrict__ row,
+                                          float none) {
+  if (V % 4 == 0 && vec) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      float4 v = make_float4(none, none, none, none);
+      if (m.first + i < m.end) v = *reinterpret_cast<const float4*>(row + m.first + i);
+      c[i] = v.x;
+      c[i + 1] = v.y;
+      c[i + 2] = v.z;
+      c[i + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) c[i] = m.first + i < m.end ? row[m.first + i] : none;
+  }
+}
+
+// The two largest c of the lane's group in b1, b2 (NaN left out).
+template <int W, int V>
+__device__ __forceinline__ void group_best(const TeamMap& m, const float (&c)[V], float* b1, float* b2) {
+  float x = c[0], y = -INFINITY;
+#pragma unroll
+  for (int i = 1; i < V; ++i) {
+    y = __builtin_amdgcn_fmed3f(x, y, c[i]);  // x >= y: the middle one is the new second
+    x = fmaxf(x, c[i]);
+  }
+  for (int off = 1; off < m.lpg; off <<= 1) {
+    const float o1 = __shfl_xor(x, off, W), o2 = __shfl_xor(y, off, W);
+    y = fmaxf(__builtin_amdgcn_fmed3f(x, y, o1), o2);
+    x = fmaxf(x, o1);
+  }
+  *b1 = x;
+  *b2 = y;
+}
+template <int W, int V>
+__device__ __forceinline__ void group_best(const TeamMap& m, const double (&c)[V], double* b1, double* b2) {
+  const auto maxr = [](double a, double b) { return a > b ? a : b; };
+  double x = -INFINITY, y = x;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int e = m.first + i * m.lpg;
-    if (e < m.end) {
-      c[i] = score(c[i]);
-      if (balance) c[i] += (R)balance[e];
-    }
+    const double v = c[i] == c[i] ? c[i] : -INFINITY;
+    y = maxr(y, v < x ? v : x);
+    x = maxr(x, v);
   }
-  const R margin = (R)(soft ? kMarginSoftmax : kMarginSigmoid);
+  for (int off = 1; off < m.lpg; off <<= 1) {
+    const double o1 = __shfl_xor(x, off, W), o2 = __shfl_xor(y, off, W);
+    y = maxr(maxr(y, o2), o1 < x ? o1 : x);
+    x = maxr(x, o1);
+  }
+  *b1 = x;
+  *b2 = y;
+}
+
+// Routing weight of the team's lane r < k from the score s of its pick.
+template <int W, class R>
+__device__ __forceinline__ R weight_of(const eb_router& p, bool mine, R s, R* sum) {
+  const R w = mine ? s : (R)0;
+  *sum = team_reduce<W>(w, [](R a, R b) { return a + b; });
+  return p.norm_topk && *sum != 0 ? w / *sum : w;
+}
+
+// The k picks of one token in fp32: lane r < k of the team returns pick r's
+// expert in *pick and its routing weight in *w.  Returns whether the token has
+// to be chosen in fp64: a decision within the error bound, values that fp32
+// comparisons do not settle (NaN, picks at -inf), or a sum of scores where fp32
+// loses digits.
+// bal: the lane's balance values, -inf where it has no expert; picks: 16 words of LDS of the team's own.
+template <bool SOFT, int W, int V>
+__device__ __forceinline__ bool choose_fp32(const eb_router& p, const TeamMap& m, int E, int k, bool vec,
+                                            const float* __restrict__ z, const float (&bal)[V], volatile int* picks,
+                                            int* pick, float* w) {
+  // max as a median: fmaxf first quiets what an exchange brings
+  const auto maxf = [](float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); };
+  const float ninf = -INFINITY;
+  float c[V];
+  load_lane(c, m, vec, z, ninf);
+  const Scores<SOFT, float> sc = row_scores<SOFT, W, V>(c);
   bool near = false;
-  // group choice
-  bool kept = m.group < p.n_group;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    c[i] = sc.of(c[i]) + bal[i];
+    near |= !(c[i] == c[i]);
+  }
+  const float margin = SOFT ? kMarginSoftmax : kMarginSigmoid, floor = 2 * margin * sc.top();
   if (p.topk_group < p.n_group) {
-    R b1 = ninf, b2 = ninf;  // the lane's, then the group's, two largest (NaN counts as -inf)
+    float b1, b2;
+    group_best<W, V>(m, c, &b1, &b2);
+    const float gs = p.group_top == 2 ? b1 + b2 : b1;
+    int before = 0;
+    for (int g = 0; g < p.n_group; ++g) before += __shfl(gs, g * m.lpg, W) > gs;
+    const bool real = m.group < p.n_group, kept = real && before < p.topk_group;
+    // the last group kept against the first left out, each at its worst
+    const float err = floor + margin * (fabsf(b1) + (p.group_top == 2 ? fabsf(b2) : 0.f));
+    const float in = team_reduce<W>(kept ? err - gs : ninf, maxf);
+    const float out = team_reduce<W>(real && !kept ? gs + err : ninf, maxf);
+    near |= !(-in > out) || (real && !(gs - gs == 0.f));
+#pragma unroll
+    for (int i = 0; i < V; ++i) c[i] = kept ? c[i] : ninf;
+  }
+  // the k largest and the one after them: lane r keeps the r-th value (lane 15
+  // none where k = 16: the last comparison is made from `best`)
+  float own = ninf, best = ninf;
+  int given = 0;
+  for (int r = 0;; ++r) {
+    float top = c[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) top = fmaxf(top, c[i]);
+    const float prev = best;
+    best = team_reduce<W>(top, maxf);
+    if (r == k) {  // the best that was not picked, if any is left
+      near |= best != ninf && !(prev - best > floor + margin * (fabsf(prev) + fabsf(best)));
+      break;
+    }
+    own = m.sub == r ? best : own;
+    // the lane that holds it gives it up.  Equal values: a second one of the
+    // same lane comes next, at a distance of 0; one of another lane is given up
+    // too and counts twice
+    bool found = false;
+    int at = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const R v = m.first + i * m.lpg < m.end && c[i] == c[i] ? c[i] : ninf;
-      b2 = maxr(b2, v < b1 ? v : b1);
-      b1 = maxr(b1, v);
+      const bool hit = c[i] == best && !found;
+      at = hit ? i : at;
+      c[i] = hit ? ninf : c[i];
+      found = found || hit;
     }
-    for (int off = 1; off < m.lpg; off <<= 1) {
-      const R o1 = __shfl_xor(b1, off, W), o2 = __shfl_xor(b2, off, W);
-      b2 = maxr(maxr(b2, o2), o1 < b1 ? o1 : b1);
-      b1 = maxr(b1, o1);
-    }
-    R gs = p.group_top == 2 ? b1 + b2 : b1;
+    if (found) picks[r] = m.first + at;
+    given += found;
+  }
+  near |= team_reduce<W>(given, [](int a, int b) { return a + b; }) != k;
+  const float before = __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(own), 0x111, 0xF, 0xF, true));
+  if (m.sub > 0 && m.sub < k) near |= !(before - own > floor + margin * (fabsf(before) + fabsf(own)));
+  if (m.sub < k) near |= own == ninf;
+  const int mine = m.sub < k ? min(max(picks[m.sub], 0), E - 1) : 0;
+  *pick = mine;
+  float sum;
+  const float we = weight_of<W>(p, m.sub < k, sc.of(z[mine]), &sum);
+  *w = we * p.scale;
+  near |= p.norm_topk && !(sum >= kTiny);
+  return team_reduce<W>((uint32_t)near, [](uint32_t a, uint32_t b) { return a | b; }) != 0;
+}
+
+// The same from fp64 scores by a whole wavefront: decided.
+template <bool SOFT, int V>
+__device__ __forceinline__ void choose_fp64(const eb_router& p, int E, int k, const float* __restrict__ z,
+                                            const float* __restrict__ balance, int* pick, float* w) {
+  const TeamMap m = team_map<64, V>(p, E, threadIdx.x & 63);
+  const auto maxk = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
+  const double ninf = -INFINITY;
+  double c[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) c[i] = m.first + i < m.end ? (double)z[m.first + i] : ninf;
+  const Scores<SOFT, double> sc = row_scores<SOFT, 64, V>(c);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = m.first + i;
+    c[i] = e < m.end ? sc.of(c[i]) + (balance ? (double)balance[e] : 0.0) : ninf;
+  }
+  bool kept = m.group < p.n_group;
+  if (p.topk_group < p.n_group) {
+    double b1, b2;
+    group_best<64, V>(m, c, &b1, &b2);
+    double gs = p.group_top == 2 ? b1 + b2 : b1;
     if (!(gs == gs)) gs = ninf;
     int before = 0;
     for (int g = 0; g < p.n_group; ++g) {
-      const R o = __shfl(gs, g * m.lpg, W);
+      const double o = __shfl(gs, g * m.lpg, 64);
       before += o > gs || (o == gs && g < m.group);
     }
-    const bool real = kept;
-    kept = real && before < p.topk_group;
-    // the last group kept against the first left out, each at its worst
-    const R err = gs - gs == 0 ? margin * (2 * top + magnitude(b1) + (p.group_top == 2 ? magnitude(b2) : 0)) : 0;
-    const R in = team_reduce<W>(kept ? err - gs : ninf, maxr);
-    const R out = team_reduce<W>(real && !kept ? gs + err : ninf, maxr);
-    if (!(-in > out)) near = true;
+    kept = kept && before < p.topk_group;
   }
-  Key key[V];
+  uint64_t key[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) key[i] = kept && m.first + i * m.lpg < m.end ? order_key(c[i]) : (Key)0;
-  R last = 0;
-  const bool more = k < E;
+  for (int i = 0; i < V; ++i) key[i] = kept && m.first + i < m.end ? order_key(c[i]) : 0ull;
   int mine = 0;
-  for (int r = 0; r < k + 1; ++r) {
-    if (r == k && (sizeof(R) == 8 || !more)) break;
-    Key best = 0;
+  for (int r = 0; r < k; ++r) {
+    uint64_t best = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) best = maxk(best, key[i]);
-    best = team_reduce<W>(best, maxk);
-    if constexpr (sizeof(R) == 4) {
-      const R v = key_float(best);
-      // equal or close values, NaN and no value at all (the extra round's) alike
-      if (r > 0 && best != 0 && !(last - v > margin * (2 * top + magnitude(last) + magnitude(v)))) near = true;
-      last = v;
-    }
-    if (r == k) break;
-    uint32_t at = ~0u;
+    best = team_reduce<64>(best, maxk);
+    int lane_at = 0x7fffffff;
 #pragma unroll
     for (int i = V - 1; i >= 0; --i)
-      if (key[i] == best) at = (uint32_t)(m.first + i * m.lpg);
-    const uint32_t lane_at = at;
-    at = team_reduce<W>(at, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+      if (key[i] == best) lane_at = m.first + i;
+    const int at = team_reduce<64>(lane_at, [](int a, int b) { return a < b ? a : b; });
     if (lane_at == at) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        if (m.first + i * m.lpg == (int)at) key[i] = 0;
+        if (m.first + i == at) key[i] = 0;
     }
-    if (m.sub == r) mine = (int)at;
+    if (m.sub == r) mine = at;
   }
-  mine = min(max(mine, 0), E - 1);
-  R weight = m.sub < k ? score((R)z[mine]) : (R)0;
-  if (p.norm_topk) {
-    const R sum = team_reduce<W>(weight, [](R a, R b) { return a + b; });
-    if (sum != 0) weight = weight / sum;
-    near = near || sum < (R)kTiny;
-  }
-  *pick = mine;
-  *w = (float)weight * p.scale;
-  *close = near;
+  *pick = mine = min(max(mine, 0), E - 1);
+  double sum;
+  *w = (float)weight_of<64>(p, m.sub < k, sc.of((double)z[mine]), &sum) * p.scale;
 }
 
-// One workgroup per 32-token block of the batch.  OWN: every entry of the batch
-// has one block, whose workgroup writes the entry's counts; else they were
-// cleared before and are added to.
+// SUB workgroups of TH threads per 32-token block of the batch; VX experts a
+// lane in the fp64 choice.  OWN (SUB 1): every entry of the batch has one block, whose
+// workgroup writes the entry's counts; else they were cleared before and are
+// added to.
 constexpr int kSelectTokens = 32;
-template <int W, int V, bool OWN, class RBA>
-__global__ __launch_bounds__(256) void select_kernel(RBA rba, eb_router p, int E, int k) {
+template <bool SOFT, int W, int V, int VX, int TH, int SUB, bool OWN, class RBA>
+__global__ __launch_bounds__(TH) void select_kernel(RBA rba, eb_router p, int E, int k) {
   __shared__ int hist[1024];
+  __shared__ int picks[TH / W][kMaxSlots];
   const RouteBatch& rb = rba.get();
   if ((int)blockIdx.x >= rb.blk0[rb.n]) return;  // past the live blocks
   const int ei = find_entry(rb.blk0, rb.n, blockIdx.x);
-  const int t0 = (blockIdx.x - rb.blk0[ei]) * kSelectTokens;
-  const int rows = min(rb.tok0[ei + 1] - rb.tok0[ei] - t0, kSelectTokens);
+  const int t0 = (blockIdx.x - rb.blk0[ei]) * kSelectTokens + blockIdx.y * (kSelectTokens / SUB);
+  const int rows = min(rb.tok0[ei + 1] - rb.tok0[ei] - t0, kSelectTokens / SUB);
+  if (rows <= 0) return;
   const float* __restrict__ z = in_global(static_cast<const float*>(rb.e[ei].z)) + (size_t)t0 * E;
   const float* __restrict__ balance = in_global(rb.e[ei].balance);
   int32_t* __restrict__ idx = in_global(rb.e[ei].idx) + (size_t)t0 * k;
   float* __restrict__ w = in_global(rb.e[ei].w) + (size_t)t0 * k;
-  for (int e = threadIdx.x; e < E; e += 256) hist[e] = 0;
+  for (int e = threadIdx.x; e < E; e += TH) hist[e] = 0;
   __syncthreads();
-  TeamMap m;
-  m.sub = threadIdx.x % W;
-  m.lpg = W;
-  while (m.lpg * p.n_group > W) m.lpg >>= 1;
-  m.group = m.sub / m.lpg;
-  const int M = E / p.n_group;
-  m.first = m.group * M + m.sub % m.lpg;
-  m.end = m.group < p.n_group ? (m.group + 1) * M : 0;
-  // whole teams leave the loop together, but not all teams of a wavefront: the
-  // exchanges stay within a team
-  for (int t = threadIdx.x / W; t < rows; t += 256 / W) {
+  const TeamMap m = team_map<W, V>(p, E, threadIdx.x % W);
+  // rows, groups and lanes start on 16 bytes
+  const bool vec = E % 4 == 0 && (E / p.n_group) % 4 == 0 && (reinterpret_cast<uintptr_t>(z) & 15) == 0;
+  float bal[V];
+  if (balance) load_lane(bal, m, vec && (reinterpret_cast<uintptr_t>(balance) & 15) == 0, balance, -INFINITY);
+  else
+#pragma unroll
+    for (int i = 0; i < V; ++i) bal[i] = m.first + i < m.end ? 0.f : -INFINITY;
+  auto store = [&](int t, int r, int e, float we) {
+    idx[(size_t)t * k + r] = e;
+    w[(size_t)t * k + r] = we;
+    atomicAdd(&hist[e], 1);
+  };
+  // a wavefront's tokens at t .. t + 64 / W - 1: its teams stay together
+  constexpr int PER = 64 / W, STEP = TH / W;
+  for (int t = (threadIdx.x >> 6) * PER; t < rows; t += STEP) {
+    const int tt = t + (threadIdx.x & 63) / W;
+    const bool live = tt < rows;
     int e;
     float we;
-    bool close;
-    const float* zt = z + (size_t)t * E;
-    choose<W, V, float>(p, m, E, k, zt, balance, &e, &we, &close);
-    if (team_reduce<W>((uint32_t)close, [](uint32_t a, uint32_t b) { return a | b; }))
-      choose<W, V, double>(p, m, E, k, zt, balance, &e, &we, &close);
-    if (m.sub < k) {
-      idx[(size_t)t * k + m.sub] = e;
-      w[(size_t)t * k + m.sub] = we;
-      atomicAdd(&hist[e], 1);
+    const bool again = choose_fp32<SOFT, W, V>(p, m, E, k, vec, z + (size_t)min(tt, rows - 1) * E, bal,
+                                         picks[threadIdx.x / W], &e, &we);
+    if (live && !again && m.sub < k) store(tt, m.sub, e, we);
+    unsigned long long left = __ballot(live && again && m.sub == 0);
+    while (left) {
+      const int tx = t + (__ffsll(left) - 1) / W;
+      left &= left - 1;
+      choose_fp64<SOFT, VX>(p, E, k, z + (size_t)tx * E, balance, &e, &we);
+      if ((int)(threadIdx.x & 63) < k) store(tx, threadIdx.x & 63, e, we);
     }
   }
   __syncthreads();
   int32_t* __restrict__ counts = in_global(rb.e[ei].counts);
-  for (int e = threadIdx.x; e < E; e += 256) {
+  for (int e = threadIdx.x; e < E; e += TH) {
     if (OWN) counts[e] = hist[e];
     else if (hist[e]) atomicAdd(&counts[e], hist[e]);
   }
@@ -289,21 +425,29 @@ __global__ __launch_bounds__(256) void counts_clear_kernel(RBA rba, int E) {
   for (int e = threadIdx.x; e < E; e += 256) counts[e] = 0;
 }
 
-template <int W, int V, class RBA>
-void select_launch_v(RBA rba, const eb_router& p, int E, int k, int grid, bool own, hipStream_t s) {
+template <bool SOFT, int W, int V, int VX, int TH, int SUB, class RBA>
+void select_launch_s(RBA rba, const eb_router& p, int E, int k, int grid, bool own, hipStream_t s) {
   if (own)
-    hipLaunchKernelGGL((select_kernel<W, V, true, RBA>), dim3(grid), dim3(256), 0, s, rba, p, E, k);
+    hipLaunchKernelGGL((select_kernel<SOFT, W, V, VX, TH, 1, true, RBA>), dim3(grid), dim3(TH), 0, s, rba, p, E, k);
   else
-    hipLaunchKernelGGL((select_kernel<W, V, false, RBA>), dim3(grid), dim3(256), 0, s, rba, p, E, k);
+    hipLaunchKernelGGL((select_kernel<SOFT, W, V, VX, TH, SUB, false, RBA>), dim3(grid, SUB), dim3(TH), 0, s, rba, p, E, k);
+}
+template <int W, int V, int VX, int TH, int SUB, class RBA>
+void select_launch(RBA rba, const eb_router& p, int E, int k, int grid, bool own, hipStream_t s) {
+  if (p.score == EB_SCORE_SOFTMAX) select_launch_s<true, W, V, VX, TH, SUB>(rba, p, E, k, grid, own, s);
+  else select_launch_s<false, W, V, VX, TH, SUB>(rba, p, E, k, grid, own, s);
 }
 
-// Experts a lane of a W-lane team holds.
+// Experts a lane of a W-lane team holds at most (0: more groups than lanes).
 int lane_experts(const eb_router& p, int E, int W) {
+  if (p.n_group > W) return 0;
   int lpg = W;
-  while (lpg > 1 && lpg * p.n_group > W) lpg >>= 1;
-  const int M = E / p.n_group;
-  return lpg * p.n_group > W ? 1 << 20 : (M + lpg - 1) / lpg;
+  while (lpg * p.n_group > W) lpg >>= 1;
+  return (E / p.n_group + lpg - 1) / lpg;
 }
+
+// Most 32-token blocks for which a token gets a whole wavefront.
+constexpr int kWholeWaveBlocks = 256;
 
 template <class RBA>
 hipError_t select_batch(RBA rba, const eb_router& p, int E, int k, int grid_entries, int grid_blocks, bool own,
@@ -312,12 +456,22 @@ hipError_t select_batch(RBA rba, const eb_router& p, int E, int k, int grid_entr
   if (!own && grid_entries > 0)
     hipLaunchKernelGGL((counts_clear_kernel<RBA>), dim3(grid_entries), dim3(256), 0, s, rba, E);
   if (grid_blocks > 0) {
+    // a lane's 16 experts in a quarter of a wavefront are at most 4 in a whole one
     const int v16 = lane_experts(p, E, 16), v64 = lane_experts(p, E, 64);
-    if (v16 <= 4) select_launch_v<16, 4>(rba, p, E, k, grid_blocks, own, s);
-    else if (v16 <= 8) select_launch_v<16, 8>(rba, p, E, k, grid_blocks, own, s);
-    else if (v16 <= 16) select_launch_v<16, 16>(rba, p, E, k, grid_blocks, own, s);
-    else if (v64 <= 8) select_launch_v<64, 8>(rba, p, E, k, grid_blocks, own, s);
-    else select_launch_v<64, 32>(rba, p, E, k, grid_blocks, own, s);
+    if (grid_blocks <= kWholeWaveBlocks && v64 <= 4) {
+      if (v64 <= 1) select_launch<64, 1, 1, 1024, 2>(rba, p, E, k, grid_blocks, own, s);
+      else select_launch<64, 4, 4, 1024, 2>(rba, p, E, k, grid_blocks, own, s);
+    } else if (v16 > 0 && v16 <= 4) {
+      select_launch<16, 4, 4, 256, 1>(rba, p, E, k, grid_blocks, own, s);
+    } else if (v16 > 0 && v16 <= 8) {
+      select_launch<16, 8, 4, 256, 1>(rba, p, E, k, grid_blocks, own, s);
+    } else if (v16 > 0 && v16 <= 16) {
+      select_launch<16, 16, 4, 256, 1>(rba, p, E, k, grid_blocks, own, s);
+    } else if (v64 <= 8) {
+      select_launch<64, 8, 8, 256, 1>(rba, p, E, k, grid_blocks, own, s);
+    } else {
+      select_launch<64, 32, 32, 256, 1>(rba, p, E, k, grid_blocks, own, s);
+    }
   }
   prof_stop(EB_K_ROUTE_TOPK, s);
   return hipGetLastError();

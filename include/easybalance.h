@@ -211,7 +211,7 @@ typedef struct eb_router {
 
 /*
  * easybalance_select -- experts, weights and counts of T tokens from their
- * router logits, under `router` (see eb_router).  One launch for up to 32
+ * router logits, under `router` (see eb_router).  One launch for up to 16
  * tokens, else two.
  *
  * logits     device [T][E] fp32

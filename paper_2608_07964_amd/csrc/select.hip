@@ -32,12 +32,13 @@
 namespace eb {
 namespace {
 
-// Bounds of the error of c in fp32, relative to (largest s of the row + |c|).
-// Sigmoid: s(1-s)|z| < 0.23 bounds what the rounded exponent does to s, exp2,
-// the sum and the reciprocal add an ulp each, s + balance half an ulp: below
-// 2^-22.  Softmax: its denominator is a sum of E <= 1024 terms, 32 in a lane
-// and then 6 levels: 38 roundings and the exponential's, below 2^-18.
-constexpr float kMarginSigmoid = 0x1p-21f, kMarginSoftmax = 0x1p-17f;
+// Bounds of the error of s in fp32, relative to the row's largest s (1 for
+// sigmoids), and of s + balance, relative to the result.  Sigmoid, in units of
+// 2^-24: the exponent's product, s(1-s)|z| 1.25 < 0.3; exp2, one ulp, 0.5; 1 + e,
+// 1; the reciprocal, one ulp, 2: together below 2^-22.  Softmax: its denominator
+// is a sum of E <= 1024 terms, 32 in a lane and then 6 levels: 38 roundings and
+// the exponential's, below 2^-18.
+constexpr float kMarginSigmoid = 0x1p-22f, kMarginSoftmax = 0x1p-18f, kMarginSum = 0x1p-24f;
 // Sums of the picked scores below this are formed in fp64 (fp32 scores near
 // its smallest numbers have few digits).
 constexpr float kTiny = 1e-30f;
@@ -176,23 +177,7 @@ __device__ __forceinline__ void load_lane(float (&c)[V], const TeamMap& m, bool 
   }
 }
 
-// The two largest c of the lane's group in b1, b2 (NaN left out).
-template <int W, int V>
-__device__ __forceinline__ void group_best(const TeamMap& m, const float (&c)[V], float* b1, float* b2) {
-  float x = c[0], y = -INFINITY;
-#pragma unroll
-  for (int i = 1; i < V; ++i) {
-    y = __builtin_amdgcn_fmed3f(x, y, c[i]);  // x >= y: the middle one is the new second
-    x = fmaxf(x, c[i]);
-  }
-  for (int off = 1; off < m.lpg; off <<= 1) {
-    const float o1 = __shfl_xor(x, off, W), o2 = __shfl_xor(y, off, W);
-    y = fmaxf(__builtin_amdgcn_fmed3f(x, y, o1), o2);
-    x = fmaxf(x, o1);
-  }
-  *b1 = x;
-  *b2 = y;
-}
+// The two largest c of the lane's group in b1, b2 (NaN counts as -inf).
 template <int W, int V>
 __device__ __forceinline__ void group_best(const TeamMap& m, const double (&c)[V], double* b1, double* b2) {
   const auto maxr = [](double a, double b) { return a > b ? a : b; };
@@ -220,83 +205,123 @@ __device__ __forceinline__ R weight_of(const eb_router& p, bool mine, R s, R* su
   return p.norm_topk && *sum != 0 ? w / *sum : w;
 }
 
+// Unsigned key of a value's order with its place among the lane's V values in
+// the low SLOT bits, and the largest value that has the key (at most ERROR of its
+// magnitude larger).  LOWEST: -inf; 0 is no value.
+template <int V>
+struct SlotKey {
+  static constexpr int SLOT = V <= 4 ? 2 : V <= 8 ? 3 : V <= 16 ? 4 : 5;
+  static constexpr uint32_t MASK = (1u << SLOT) - 1;
+  static constexpr float ERROR = 1.f / (1 << (23 - SLOT));
+  static constexpr uint32_t LOWEST = 0x007fffffu;  // -inf with every slot bit set
+  static __device__ __forceinline__ uint32_t of(float v, int i) {
+    const uint32_t u = __float_as_uint(v);
+    const uint32_t o = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+    return (o & ~MASK) | (uint32_t)i;
+  }
+  static __device__ __forceinline__ float value(uint32_t key) {
+    const uint32_t o = key | MASK;
+    return __uint_as_float(o ^ ((o & 0x80000000u) ? 0x80000000u : 0xffffffffu));
+  }
+};
+
+// Sorts the lane's keys, largest first (odd-even merges).
+template <int V>
+__device__ __forceinline__ void sort_lane(uint32_t (&a)[V]) {
+#pragma unroll
+  for (int p = 1; p < V; p *= 2)
+#pragma unroll
+    for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+      for (int j = q % p; j + q < V; j += 2 * q)
+#pragma unroll
+        for (int i = 0; i < q; ++i)
+          if (i + j + q < V && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+            const uint32_t hi = max(a[i + j], a[i + j + q]), lo = min(a[i + j], a[i + j + q]);
+            a[i + j] = hi;
+            a[i + j + q] = lo;
+          }
+}
+
 // The k picks of one token in fp32: lane r < k of the team returns pick r's
 // expert in *pick and its routing weight in *w.  Returns whether the token has
 // to be chosen in fp64: a decision within the error bound, values that fp32
-// comparisons do not settle (NaN, picks at -inf), or a sum of scores where fp32
-// loses digits.
-// bal: the lane's balance values, -inf where it has no expert; picks: 16 words of LDS of the team's own.
-template <bool SOFT, int W, int V>
-__device__ __forceinline__ bool choose_fp32(const eb_router& p, const TeamMap& m, int E, int k, bool vec,
-                                            const float* __restrict__ z, const float (&bal)[V], volatile int* picks,
-                                            int* pick, float* w) {
+// comparisons do not settle (NaN, infinities), or a sum of scores where fp32
+// loses digits.  c: the lane's logits, -inf where it has no expert; bal: its
+// balance values, -inf there; picks: 16 words of LDS of the team's own; DEPTH:
+// how many of its values a lane can give up, at least min(V, k + 1).
+template <bool SOFT, int W, int V, int DEPTH>
+__device__ __forceinline__ bool choose_fp32(const eb_router& p, const TeamMap& m, int E, int k,
+                                            const float* __restrict__ z, const float* __restrict__ balance,
+                                            const float (&c)[V], const float (&bal)[V],
+                                            volatile int* picks, int* pick, float* w) {
+  using Key = SlotKey<V>;
   // max as a median: fmaxf first quiets what an exchange brings
   const auto maxf = [](float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); };
+  const auto maxk = [](uint32_t a, uint32_t b) { return max(a, b); };
   const float ninf = -INFINITY;
-  float c[V];
-  load_lane(c, m, vec, z, ninf);
   const Scores<SOFT, float> sc = row_scores<SOFT, W, V>(c);
   bool near = false;
+  uint32_t key[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    c[i] = sc.of(c[i]) + bal[i];
-    near |= !(c[i] == c[i]);
+    const float v = sc.of(c[i]) + bal[i];
+    near |= !(v < INFINITY);
+    key[i] = Key::of(v, i);
   }
-  const float margin = SOFT ? kMarginSoftmax : kMarginSigmoid, floor = 2 * margin * sc.top();
+  sort_lane(key);
+  // x and y are close where |x - y| <= floor + kMarginSum (|x| + |y|)
+  const float floor = 2 * (SOFT ? kMarginSoftmax : kMarginSigmoid) * sc.top();
   if (p.topk_group < p.n_group) {
-    float b1, b2;
-    group_best<W, V>(m, c, &b1, &b2);
-    const float gs = p.group_top == 2 ? b1 + b2 : b1;
+    float x = Key::value(key[0]), y = V > 1 ? Key::value(key[V > 1 ? 1 : 0]) : ninf;
+    for (int off = 1; off < m.lpg; off <<= 1) {
+      const float o1 = __shfl_xor(x, off, W), o2 = __shfl_xor(y, off, W);
+      y = fmaxf(__builtin_amdgcn_fmed3f(x, y, o1), o2);
+      x = fmaxf(x, o1);
+    }
+    const float gs = p.group_top == 2 ? x + y : x;
     int before = 0;
     for (int g = 0; g < p.n_group; ++g) before += __shfl(gs, g * m.lpg, W) > gs;
     const bool real = m.group < p.n_group, kept = real && before < p.topk_group;
     // the last group kept against the first left out, each at its worst
-    const float err = floor + margin * (fabsf(b1) + (p.group_top == 2 ? fabsf(b2) : 0.f));
-    const float in = team_reduce<W>(kept ? err - gs : ninf, maxf);
+    const float size = fabsf(x) + (p.group_top == 2 ? fabsf(y) : 0.f), err = floor + 2 * kMarginSum * size;
+    const float in = team_reduce<W>(kept ? err + Key::ERROR * size - gs : ninf, maxf);
     const float out = team_reduce<W>(real && !kept ? gs + err : ninf, maxf);
     near |= !(-in > out) || (real && !(gs - gs == 0.f));
 #pragma unroll
-    for (int i = 0; i < V; ++i) c[i] = kept ? c[i] : ninf;
+    for (int i = 0; i < DEPTH; ++i) key[i] = kept ? key[i] : 0u;
   }
-  // the k largest and the one after them: lane r keeps the r-th value (lane 15
-  // none where k = 16: the last comparison is made from `best`)
-  float own = ninf, best = ninf;
+  // the k largest keys and the one after them
   int given = 0;
+  uint32_t best;
   for (int r = 0;; ++r) {
-    float top = c[0];
-#pragma unroll
-    for (int i = 1; i < V; ++i) top = fmaxf(top, c[i]);
-    const float prev = best;
-    best = team_reduce<W>(top, maxf);
-    if (r == k) {  // the best that was not picked, if any is left
-      near |= best != ninf && !(prev - best > floor + margin * (fabsf(prev) + fabsf(best)));
-      break;
-    }
-    own = m.sub == r ? best : own;
-    // the lane that holds it gives it up.  Equal values: a second one of the
-    // same lane comes next, at a distance of 0; one of another lane is given up
-    // too and counts twice
-    bool found = false;
-    int at = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const bool hit = c[i] == best && !found;
-      at = hit ? i : at;
-      c[i] = hit ? ninf : c[i];
-      found = found || hit;
-    }
-    if (found) picks[r] = m.first + at;
+    best = team_reduce<W>(key[0], maxk);
+    if (r == k) break;
+    // the lane that holds it gives it up (two that do count twice)
+    const bool found = key[0] == best;
+    if (found) picks[r] = m.first + (int)(best & Key::MASK);
     given += found;
+    near |= best <= Key::LOWEST;
+    // (as masks: a choice between neighbours of an array becomes a search for
+    // an index that is not constant)
+    const uint32_t pop = found ? ~0u : 0u;
+#pragma unroll
+    for (int i = 0; i + 1 < DEPTH; ++i) key[i] = (key[i + 1] & pop) | (key[i] & ~pop);
+    key[DEPTH - 1] &= ~pop;
   }
   near |= team_reduce<W>(given, [](int a, int b) { return a + b; }) != k;
-  const float before = __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(own), 0x111, 0xF, 0xF, true));
-  if (m.sub > 0 && m.sub < k) near |= !(before - own > floor + margin * (fabsf(before) + fabsf(own)));
-  if (m.sub < k) near |= own == ninf;
-  const int mine = m.sub < k ? min(max(picks[m.sub], 0), E - 1) : 0;
-  *pick = mine;
+  // lane r has pick r: its value against the one before, the last one against
+  // the best that was not picked
+  const bool mine = m.sub < k;
+  const int e = mine ? min(max(picks[m.sub], 0), E - 1) : 0;
+  const float s = sc.of(z[e]), v = s + (balance ? balance[e] : 0.f);
+  const float u = __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x111, 0xF, 0xF, true));
+  if (m.sub > 0 && mine) near |= !(u - v > floor + kMarginSum * (fabsf(u) + fabsf(v)));
+  const float rest = Key::value(best);
+  if (m.sub == k - 1) near |= best > Key::LOWEST && !(v - rest > floor + kMarginSum * (fabsf(v) + fabsf(rest)));
+  *pick = e;
   float sum;
-  const float we = weight_of<W>(p, m.sub < k, sc.of(z[mine]), &sum);
-  *w = we * p.scale;
+  *w = weight_of<W>(p, mine, s, &sum) * p.scale;
   near |= p.norm_topk && !(sum >= kTiny);
   return team_reduce<W>((uint32_t)near, [](uint32_t a, uint32_t b) { return a | b; }) != 0;
 }
@@ -356,21 +381,29 @@ __device__ __forceinline__ void choose_fp64(const eb_router& p, int E, int k, co
   *w = (float)weight_of<64>(p, m.sub < k, sc.of((double)z[mine]), &sum) * p.scale;
 }
 
-// SUB workgroups of TH threads per 32-token block of the batch; VX experts a
-// lane in the fp64 choice.  OWN (SUB 1): every entry of the batch has one block, whose
-// workgroup writes the entry's counts; else they were cleared before and are
-// added to.
-constexpr int kSelectTokens = 32;
-template <bool SOFT, int W, int V, int VX, int TH, int SUB, bool OWN, class RBA>
+// A workgroup of TH threads takes TOK tokens of an entry (tiles of an entry in
+// order, entries in order); VX: experts a lane holds in the fp64 choice.  OWN
+// (every entry of the batch has 1 to TOK tokens): the workgroup writes the entry's
+// counts; else they were cleared before and are added to.  Those atomics
+// are what a large launch waits for: 32768 tokens on 256 experts took 28.7 us in
+// 32-token workgroups (19.1 without them).
+template <bool SOFT, int W, int V, int DEPTH, int VX, int TH, int TOK, bool OWN, class RBA>
 __global__ __launch_bounds__(TH) void select_kernel(RBA rba, eb_router p, int E, int k) {
   __shared__ int hist[1024];
   __shared__ int picks[TH / W][kMaxSlots];
   const RouteBatch& rb = rba.get();
-  if ((int)blockIdx.x >= rb.blk0[rb.n]) return;  // past the live blocks
-  const int ei = find_entry(rb.blk0, rb.n, blockIdx.x);
-  const int t0 = (blockIdx.x - rb.blk0[ei]) * kSelectTokens + blockIdx.y * (kSelectTokens / SUB);
-  const int rows = min(rb.tok0[ei + 1] - rb.tok0[ei] - t0, kSelectTokens / SUB);
-  if (rows <= 0) return;
+  int ei = -1, t0 = 0;
+  for (int i = 0, base = 0; i < rb.n; ++i) {
+    const int nt = (rb.tok0[i + 1] - rb.tok0[i] + TOK - 1) / TOK;
+    if ((int)blockIdx.x < base + nt) {
+      ei = i;
+      t0 = ((int)blockIdx.x - base) * TOK;
+      break;
+    }
+    base += nt;
+  }
+  if (ei < 0) return;  // past the live tiles
+  const int rows = min(rb.tok0[ei + 1] - rb.tok0[ei] - t0, TOK);
   const float* __restrict__ z = in_global(static_cast<const float*>(rb.e[ei].z)) + (size_t)t0 * E;
   const float* __restrict__ balance = in_global(rb.e[ei].balance);
   int32_t* __restrict__ idx = in_global(rb.e[ei].idx) + (size_t)t0 * k;
@@ -390,15 +423,23 @@ __global__ __launch_bounds__(TH) void select_kernel(RBA rba, eb_router p, int E,
     w[(size_t)t * k + r] = we;
     atomicAdd(&hist[e], 1);
   };
-  // a wavefront's tokens at t .. t + 64 / W - 1: its teams stay together
+  // a wavefront's tokens at t .. t + 64 / W - 1: its teams stay together.  The
+  // next ones' logits are on their way while these are chosen.
   constexpr int PER = 64 / W, STEP = TH / W;
-  for (int t = (threadIdx.x >> 6) * PER; t < rows; t += STEP) {
-    const int tt = t + (threadIdx.x & 63) / W;
+  const int first = (threadIdx.x >> 6) * PER, own = (threadIdx.x & 63) / W;
+  float c[V], next[V];
+  auto row = [&](int t) { return z + (size_t)min(t + own, rows - 1) * E; };
+  if (first < rows) load_lane(next, m, vec, row(first), -INFINITY);
+  for (int t = first; t < rows; t += STEP) {
+    const int tt = t + own;
     const bool live = tt < rows;
+#pragma unroll
+    for (int i = 0; i < V; ++i) c[i] = next[i];
+    if (t + STEP < rows) load_lane(next, m, vec, row(t + STEP), -INFINITY);
     int e;
     float we;
-    const bool again = choose_fp32<SOFT, W, V>(p, m, E, k, vec, z + (size_t)min(tt, rows - 1) * E, bal,
-                                         picks[threadIdx.x / W], &e, &we);
+    const bool again = choose_fp32<SOFT, W, V, DEPTH>(p, m, E, k, row(t), balance, c, bal,
+                                                      picks[threadIdx.x / W], &e, &we);
     if (live && !again && m.sub < k) store(tt, m.sub, e, we);
     unsigned long long left = __ballot(live && again && m.sub == 0);
     while (left) {
@@ -425,17 +466,18 @@ __global__ __launch_bounds__(256) void counts_clear_kernel(RBA rba, int E) {
   for (int e = threadIdx.x; e < E; e += 256) counts[e] = 0;
 }
 
-template <bool SOFT, int W, int V, int VX, int TH, int SUB, class RBA>
-void select_launch_s(RBA rba, const eb_router& p, int E, int k, int grid, bool own, hipStream_t s) {
-  if (own)
-    hipLaunchKernelGGL((select_kernel<SOFT, W, V, VX, TH, 1, true, RBA>), dim3(grid), dim3(TH), 0, s, rba, p, E, k);
-  else
-    hipLaunchKernelGGL((select_kernel<SOFT, W, V, VX, TH, SUB, false, RBA>), dim3(grid, SUB), dim3(TH), 0, s, rba, p, E, k);
+template <bool SOFT, int W, int V, int DEPTH, int VX, int TH, int TOK, bool OWN, class RBA>
+void select_launch_o(RBA rba, const eb_router& p, int E, int k, int entries, int blocks, hipStream_t s) {
+  // tiles of TOK tokens: at most one more an entry than the 32-token blocks make
+  const int grid = OWN ? entries : TOK <= 32 ? blocks * (32 / TOK) : blocks / (TOK / 32) + entries;
+  hipLaunchKernelGGL((select_kernel<SOFT, W, V, DEPTH, VX, TH, TOK, OWN, RBA>), dim3(grid), dim3(TH), 0, s, rba, p, E, k);
 }
-template <int W, int V, int VX, int TH, int SUB, class RBA>
-void select_launch(RBA rba, const eb_router& p, int E, int k, int grid, bool own, hipStream_t s) {
-  if (p.score == EB_SCORE_SOFTMAX) select_launch_s<true, W, V, VX, TH, SUB>(rba, p, E, k, grid, own, s);
-  else select_launch_s<false, W, V, VX, TH, SUB>(rba, p, E, k, grid, own, s);
+template <int W, int V, int DEPTH, int VX, int TH, int TOK, bool OWN, class RBA>
+void select_launch(RBA rba, const eb_router& p, int E, int k, int entries, int blocks, hipStream_t s) {
+  if (p.score == EB_SCORE_SOFTMAX)
+    select_launch_o<true, W, V, DEPTH, VX, TH, TOK, OWN>(rba, p, E, k, entries, blocks, s);
+  else
+    select_launch_o<false, W, V, DEPTH, VX, TH, TOK, OWN>(rba, p, E, k, entries, blocks, s);
 }
 
 // Experts a lane of a W-lane team holds at most (0: more groups than lanes).
@@ -446,8 +488,32 @@ int lane_experts(const eb_router& p, int E, int W) {
   return (E / p.n_group + lpg - 1) / lpg;
 }
 
-// Most 32-token blocks for which a token gets a whole wavefront.
-constexpr int kWholeWaveBlocks = 256;
+// Most 32-token blocks for which a token gets a whole wavefront.  Calls of 256
+// experts in 8 groups, whole wavefronts / quarters, in us: 1024 tokens 9.7 / 16.8,
+// 4096 13.4 / 18.9, 6144 19.2 / 17.6, 8192 18.3 / 21.4, 12288 25.4 / 21.3, 32768
+// 53.3 / 22.0; of 64 experts: 1024 7.8 / 12.9, 4096 11.5 / 13.1, 6144 14.7 / 12.2.
+constexpr int kWholeWaveBlocks = 160;
+// Most tokens of an entry for which one workgroup takes all of them and writes
+// the counts itself: one a wavefront (32 tokens, two a wavefront, took 11.3 us,
+// 33 with the counts cleared by a launch before 8.7).
+constexpr int kOwnTokens = 16;
+
+// OWN: every entry has 1 to kOwnTokens tokens.  A token takes a whole wavefront where that
+// leaves none waiting; above, a quarter of one, which costs fewer instructions.
+template <bool OWN, class RBA>
+void select_dispatch(RBA rba, const eb_router& p, int E, int k, int entries, int blocks, hipStream_t s) {
+  // a lane's 16 experts in a quarter of a wavefront are at most 4 in a whole one
+  const int v16 = lane_experts(p, E, 16), v64 = lane_experts(p, E, 64);
+  constexpr int SMALL = 16, LARGE = OWN ? 16 : 128, TH = OWN ? 256 : 1024, REST = OWN ? 16 : 32;
+  if (blocks <= kWholeWaveBlocks && v64 <= 1) select_launch<64, 1, 1, 1, 1024, SMALL, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (blocks <= kWholeWaveBlocks && v64 <= 4) select_launch<64, 4, 4, 4, 1024, SMALL, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (v16 > 0 && v16 <= 4) select_launch<16, 4, 4, 4, TH, LARGE, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (v16 > 0 && v16 <= 8) select_launch<16, 8, 8, 4, TH, LARGE, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (v16 > 0 && v16 <= 16 && k <= 8) select_launch<16, 16, 9, 4, TH, LARGE, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (v16 > 0 && v16 <= 16) select_launch<16, 16, 16, 4, TH, LARGE, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (v64 <= 8) select_launch<64, 8, 8, 8, 256, REST, OWN>(rba, p, E, k, entries, blocks, s);
+  else select_launch<64, 32, 32, 32, 256, REST, OWN>(rba, p, E, k, entries, blocks, s);
+}
 
 template <class RBA>
 hipError_t select_batch(RBA rba, const eb_router& p, int E, int k, int grid_entries, int grid_blocks, bool own,
@@ -456,22 +522,8 @@ hipError_t select_batch(RBA rba, const eb_router& p, int E, int k, int grid_entr
   if (!own && grid_entries > 0)
     hipLaunchKernelGGL((counts_clear_kernel<RBA>), dim3(grid_entries), dim3(256), 0, s, rba, E);
   if (grid_blocks > 0) {
-    // a lane's 16 experts in a quarter of a wavefront are at most 4 in a whole one
-    const int v16 = lane_experts(p, E, 16), v64 = lane_experts(p, E, 64);
-    if (grid_blocks <= kWholeWaveBlocks && v64 <= 4) {
-      if (v64 <= 1) select_launch<64, 1, 1, 1024, 2>(rba, p, E, k, grid_blocks, own, s);
-      else select_launch<64, 4, 4, 1024, 2>(rba, p, E, k, grid_blocks, own, s);
-    } else if (v16 > 0 && v16 <= 4) {
-      select_launch<16, 4, 4, 256, 1>(rba, p, E, k, grid_blocks, own, s);
-    } else if (v16 > 0 && v16 <= 8) {
-      select_launch<16, 8, 4, 256, 1>(rba, p, E, k, grid_blocks, own, s);
-    } else if (v16 > 0 && v16 <= 16) {
-      select_launch<16, 16, 4, 256, 1>(rba, p, E, k, grid_blocks, own, s);
-    } else if (v64 <= 8) {
-      select_launch<64, 8, 8, 256, 1>(rba, p, E, k, grid_blocks, own, s);
-    } else {
-      select_launch<64, 32, 32, 256, 1>(rba, p, E, k, grid_blocks, own, s);
-    }
+    if (own) select_dispatch<true>(rba, p, E, k, grid_entries, grid_blocks, s);
+    else select_dispatch<false>(rba, p, E, k, grid_entries, grid_blocks, s);
   }
   prof_stop(EB_K_ROUTE_TOPK, s);
   return hipGetLastError();
@@ -481,14 +533,17 @@ hipError_t select_batch(RBA rba, const eb_router& p, int E, int k, int grid_entr
 
 hipError_t launch_select_batch(const eb_router& p, int E, int k, const RouteBatch& rb, hipStream_t s) {
   bool one = true;
-  for (int i = 0; i < rb.n; ++i) one = one && rb.blk0[i + 1] - rb.blk0[i] == 1;
+  for (int i = 0; i < rb.n; ++i) {
+    const int T = rb.tok0[i + 1] - rb.tok0[i];
+    one = one && T >= 1 && T <= kOwnTokens;
+  }
   return select_batch(ByValue<RouteBatch>{rb}, p, E, k, rb.n, rb.blk0[rb.n], one, s);
 }
 
 hipError_t launch_select_batch_dev(const eb_router& p, int E, int k, const RouteBatch* rb, int max_entries, int T,
                                    hipStream_t s) {
-  return select_batch(InMemory<RouteBatch>{rb}, p, E, k, max_entries, max_entries * ((T + 31) / 32), T >= 1 && T <= 32,
-                      s);
+  return select_batch(InMemory<RouteBatch>{rb}, p, E, k, max_entries, max_entries * ((T + 31) / 32),
+                      T >= 1 && T <= kOwnTokens, s);
 }
 
 }  // namespace eb

@@ -66,10 +66,18 @@ def test_shapes(shape, score):
               n_group=G, topk_group=TG, group_top=top, norm_topk=norm, scale=scale)
 
 
-@pytest.mark.parametrize("T", [0, 1, 31, 32, 33, 64, 257, 1000])
+@pytest.mark.parametrize("T", [0, 1, 15, 16, 17, 32, 33, 64, 257, 1000, 5119, 5121, 8200])
 def test_token_counts(T):
     rng = np.random.default_rng(T)
-    check(rng.normal(size=(T, 256)), 8, balance=rng.normal(size=256) * 0.05, score="sigmoid", n_group=8, topk_group=4)
+    z, bal = rng.normal(size=(T, 256)).astype(np.float32), (rng.normal(size=256) * 0.05).astype(np.float32)
+    kw = dict(balance=bal, score="sigmoid", n_group=8, topk_group=4)
+    if T <= 1000:
+        return check(z, 8, **kw)
+    idx, w, counts = run_select(z, 8, **kw)
+    assert np.array_equal(counts, np.bincount(idx.reshape(-1), minlength=256))
+    rows = np.r_[:100, T - 100:T]
+    want = o8.select(z[rows], 8, **kw)
+    assert np.array_equal(idx[rows], want[0]) and np.allclose(w[rows], want[1], rtol=W_REL, atol=0)
 
 
 @pytest.mark.parametrize("score", ["sigmoid", "softmax"])

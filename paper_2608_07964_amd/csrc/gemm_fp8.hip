@@ -98,8 +98,10 @@ struct Frags {
   intx8 a[C::MB], b[C::NB];
 };
 
+constexpr int kNonTemporal = 2;  // bit nt of a buffer load's cache policy
+template <int POLICY = 0>
 __device__ __forceinline__ void load16_lds(__amdgpu_buffer_rsrc_t r, uint8_t* lds, int voff, int soff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 16, voff, soff, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 16, voff, soff, 0, POLICY);
 }
 template <class C>
 __device__ __forceinline__ void load_a(const KLoop& L, int s, int slot, int j) {
@@ -141,6 +143,13 @@ struct LoadOrder {
   }
   static_assert(after_next() < 64 && after_stage0() < 64, "vmcnt range");
 };
+
+// Ties a value to its place among the instructions with side effects (an empty
+// statement that claims to change it).
+template <class T>
+__device__ __forceinline__ void pin(T& v) {
+  asm volatile("" : "+v"(v));
+}
 
 // Half h (64 bytes of K) of a fragment row: 16-byte chunks 4 h + khalf and
 // 4 h + 2 + khalf, the same for both operands, so the products pair up.
@@ -306,7 +315,7 @@ __device__ __forceinline__ void stage(const KLoop& L, LoopState<C>& st, floatx16
 #pragma unroll
   for (int mb = 0; mb < NACT; ++mb)
 #pragma unroll
-    for (int nb = 0; nb < C::NB; ++nb) asm volatile("" : "+v"(acc[mb][nb]));
+    for (int nb = 0; nb < C::NB; ++nb) pin(acc[mb][nb]);
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   wait_vm<LoadOrder<C>::after_next()>();
   bar();
@@ -629,11 +638,317 @@ __global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, We
   }
 }
 
+// ---------------------------------------------------------------------------
+// Decode launches: every group has a few rows, so a launch does nothing but
+// stream the experts' weights once (see stream_gemm_bf16).  Each wavefront
+// streams a 64-weight-row column of a 256-row column tile, 8 KB a stage, with the
+// unit's up to 8 NA rows, through a ring of its own; the stages of consecutive
+// units form one sequence.  Gate/up: the four columns of a tile are 128 columns
+// of h, one scale block, so they go to the four wavefronts of a workgroup, which
+// meet once a unit to find each row's largest |h|; down: a workgroup is one
+// wavefront and meets nobody.  What a unit needs to find its rows and scales
+// (positions of the grouping, scale words) is loaded a unit ahead: a wait for it
+// would be a wait for the whole ring.
+// Each output is the same chain of operations as in grouped_gemm_fp8.
+constexpr int kStreamLds = 40 * 1024;
+template <int NA>
+struct StreamCfg {
+  static constexpr int SLOT = (NA + 8) * 1024;
+  static constexpr int FIT = kStreamLds / SLOT, R = FIT > 4 ? 4 : FIT;
+  static constexpr int LOADS = NA + 8;
+  static_assert(R >= 3 && (R - 2) * LOADS < 64, "ring");
+};
+constexpr int kStreamMinStages = 8;   // the unit's first and last R - 1 stages are apart
+constexpr int kStreamMaxStages = 128; // two scale words a lane
+
+struct StreamUnit {
+  int row0, rows, row_end;         // the chunk's first row, its rows, the end of the m-tile's rows
+  int col;                         // column tile (gate/up) or 64-row column (down)
+  const uint8_t* B;
+  const float* scales;             // of the expert's matrix
+};
+
+template <int MODE, int NA>
+__global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm_fp8(Fp8Problem p, WeightTable wt,
+                                                                                    bf16_t* __restrict__ o) {
+  using Cfg = StreamCfg<NA>;
+  constexpr int R = Cfg::R, LOADS = Cfg::LOADS, WAVES = MODE == MODE_GATEUP ? 4 : 1, NS = MODE == MODE_GATEUP ? 2 : 1;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[WAVES * kStreamLds];
+  // the ring is written by global->LDS loads the compiler does not see
+  asm volatile("" ::"v"(smem) : "memory");
+  const int lane = threadIdx.x & 63, lrow = lane & 31, khalf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint8_t* ring = smem + wave * kStreamLds;
+  const int K = MODE == MODE_GATEUP ? p.g.H : p.g.F;
+  const int n_rows = MODE == MODE_GATEUP ? 2 * p.g.F : p.g.H;
+  const int nk = K / BKB, pieces = (nk + 3) / 4;
+  const int n_cols = n_rows / (64 * WAVES);          // units of an m-tile
+  const int ES = p.g.E + p.g.S;
+  const size_t mat = (size_t)n_rows * K;
+  const int b_stage = (n_rows / BN) * (BN * BKB);    // bytes from one K stage's blocks to the next one's
+
+  const long long total = (long long)(*p.g.n_tiles) * n_cols;
+  const int xcd = blockIdx.x % kXcds, per_xcd = gridDim.x / kXcds;
+  const int u_end = (int)(((xcd + 1) * total) / kXcds);
+  auto decode = [&](int unit) {
+    StreamUnit d;
+    const int u = __builtin_amdgcn_readfirstlane(unit);
+    const int4 gd = scalar_record(p.g.tiles, u / n_cols);  // key, first row, rows, first m-tile
+    const int mt = (gd.z + BM - 1) / BM;
+    const int local = u - gd.w * n_cols;             // column, m-tile fastest
+    d.col = local / mt;
+    const int rpt = 32 * ((gd.z + 32 * mt - 1) / (32 * mt));
+    d.row0 = gd.y + (local - d.col * mt) * rpt;
+    d.row_end = min(gd.y + gd.z, d.row0 + rpt);
+    d.rows = min(8 * NA, d.row_end - d.row0);
+    const int layer = gd.x / ES, e = gd.x - layer * ES;
+    const uint8_t* W = static_cast<const uint8_t*>(MODE == MODE_GATEUP ? wt.gu[layer] : wt.dn[layer]);
+    d.B = W + e * mat;
+    d.scales = reinterpret_cast<const float*>(W + ES * mat) + e * (mat / (128 * 128));
+    return d;
+  };
+
+  // What is loaded a unit ahead: the A rows of this lane's loads and of its
+  // fragments, and its scale words (K blocks lane and 64 + lane).
+  struct Ahead {
+    int a[NA], row;
+    float word[NS][2];
+  };
+  const int lr = lane >> 3, c_even = (lane & 7) ^ (lr >> 1);
+  auto ahead = [&](const StreamUnit& d, Ahead& n) {
+#pragma unroll
+    for (int j = 0; j < NA; ++j) {
+      const int r = d.row0 + min(8 * j + lr, d.rows - 1);
+      n.a[j] = MODE == MODE_GATEUP ? p.perm[r] : r;
+    }
+    const int r = d.row0 + min(lrow, d.rows - 1);
+    n.row = MODE == MODE_GATEUP ? p.perm[r] : r;
+    const float* s = d.scales + (size_t)(MODE == MODE_GATEUP ? d.col : d.col / 2) * nk;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      n.word[i][0] = scale_word(s + (size_t)i * (p.g.F / 128) * nk, 0, nk, lane);
+      n.word[i][1] = scale_word(s + (size_t)i * (p.g.F / 128) * nk, 64, nk, lane);
+    }
+  };
+  // token of a pair (gate/up); grouped positions that no pair maps to hold anything
+  auto token = [&](int v) { return MODE == MODE_GATEUP ? min(max(v / p.slots, 0), p.tokens - 1) : v; };
+
+  // load cursor
+  const __amdgpu_buffer_rsrc_t rs = MODE == MODE_GATEUP
+      ? buffer_rsrc(p.sa, (uint32_t)(pieces * 4) * (uint32_t)p.tokens)
+      : buffer_rsrc(p.sh, (uint32_t)(pieces * 4) * (uint32_t)p.g.P);
+  const int s_stride = (MODE == MODE_GATEUP ? p.tokens : p.g.P) * 4;
+  __amdgpu_buffer_rsrc_t ra, rb;
+  int a_voff[NA], a_soff = 0, b_voff = 0;
+  auto aim = [&](const StreamUnit& d, const Ahead& n, bool any) {  // any false: no next unit, loads of empty buffers
+    const int base = MODE == MODE_GATEUP ? 0 : d.row0;
+    ra = buffer_rsrc(uniform((MODE == MODE_GATEUP ? p.qa : p.h) + (size_t)base * K),
+                     __builtin_amdgcn_readfirstlane(any ? (MODE == MODE_GATEUP ? p.tokens : d.rows) * K : 0));
+    rb = buffer_rsrc(uniform(d.B + (MODE == MODE_GATEUP ? (size_t)d.col * (BN * BKB) + wave * (64 * BKB)
+                                                       : (size_t)(d.col >> 2) * (BN * BKB) + (d.col & 3) * (64 * BKB))),
+                     __builtin_amdgcn_readfirstlane(any ? (nk - 1) * b_stage + 64 * BKB : 0));
+#pragma unroll
+    for (int j = 0; j < NA; ++j)
+      a_voff[j] = 8 * j + lr < d.rows ? (token(n.a[j]) - base) * K + ((j & 1) ? c_even ^ 4 : c_even) * 16 : (int)0x80000000;
+    a_soff = 0;
+    b_voff = lane * 16;
+  };
+  auto issue = [&](int slot) {
+    uint8_t* st = ring + slot * Cfg::SLOT;
+#pragma unroll
+    for (int j = 0; j < NA; ++j)
+      load16_lds(ra, st + j * 1024, a_voff[j], a_soff);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      load16_lds<kNonTemporal>(rb, st + (NA + j) * 1024, b_voff + j * 1024, 0);
+    a_soff += BKB;
+    b_voff += b_stage;
+  };
+
+  int u = (int)((xcd * total) / kXcds) + (int)(blockIdx.x / kXcds);
+  if (u >= u_end) return;
+  StreamUnit cur = decode(u);
+  Ahead next;
+  ahead(cur, next);
+  // scales of the unit being multiplied: weight words, the rows' exponents of
+  // four K blocks (sa) and of the next four (sn)
+  float word[NS][2];
+  int s_row = token(next.row) * 4;
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    word[i][0] = next.word[i][0];
+    word[i][1] = next.word[i][1];
+  }
+  int sa = __builtin_amdgcn_raw_buffer_load_b32(rs, s_row, 0, 0), sn = 0;
+  aim(cur, next, true);
+#pragma unroll
+  for (int s = 0; s < R - 1; ++s) issue(s);
+  int slot = 0;
+  floatx16 acc[2];
+  const int sw = (lrow >> 1) & 7;
+
+  for (;;) {
+    // the unit after this one: a group with more rows than the launch was sized
+    // for (a caller's token that picks an expert twice) goes on with its next rows
+    StreamUnit nxt = cur;
+    bool more = true;
+    if (cur.row0 + 8 * NA < cur.row_end) {
+      nxt.row0 += 8 * NA;
+      nxt.rows = min(8 * NA, cur.row_end - nxt.row0);
+    } else {
+      u += per_xcd;
+      more = u < u_end;
+      if (more) nxt = decode(u);
+    }
+    ahead(nxt, next);
+    WeightScales ws[NS][2];
+    float m[2] = {1.f, 1.f};
+    bool scaled = false;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      ws[i][0] = weight_scales(word[i][0], 0.f, lane);
+      ws[i][1] = weight_scales(word[i][1], __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ws[i][0].mant), 63)), lane);
+      scaled |= __any(ws[i][0].mant != 1.f || ws[i][1].mant != 1.f);
+      m[i] = __uint_as_float(__builtin_amdgcn_readlane(
+          __float_as_uint(nk > 64 ? ws[i][1].mant : ws[i][0].mant), (nk - 1) & 63));
+    }
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[nb][v] = 0.f;
+
+    // one stage: its loads have landed, the slot of the stage before is free
+    // (its fragment reads are done), the load cursor's next stage goes there.
+    // (Whatever else was loaded after them only makes the wait longer.)
+    auto step = [&](int s) {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+      wait_vm<(R - 2) * LOADS>();
+      asm volatile("" ::: "memory");
+      if ((s & 3) == 0) sn = __builtin_amdgcn_raw_buffer_load_b32(rs, s_row, ((s >> 2) + 1) * s_stride, 0);
+      issue(slot == 0 ? R - 1 : slot - 1);
+      int we[2];
+      float ratio[2];
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) {
+        const WeightScales& x = s < 64 ? ws[nb < NS ? nb : 0][0] : ws[nb < NS ? nb : 0][1];
+        we[nb] = __builtin_amdgcn_readlane(x.expo, s & 63);
+        ratio[nb] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x.ratio), s & 63));
+      }
+      if (scaled) {
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[nb][v] *= ratio[nb];
+      }
+      const uint8_t* fa = ring + slot * Cfg::SLOT + lrow * BKB;  // rows past 8 NA: other rows, results discarded
+      const uint8_t* fb = ring + slot * Cfg::SLOT + NA * 1024 + lrow * BKB;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int c0 = ((4 * h + khalf) ^ sw) * 16, c1 = ((4 * h + 2 + khalf) ^ sw) * 16;
+        const intx8 a = read_frag(fa + c0, fa + c1);
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb)
+          acc[nb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+              read_frag(fb + nb * 32 * BKB + c0, fb + nb * 32 * BKB + c1), a, acc[nb], 0, 0, 0, we[nb], 0, sa);
+      }
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) pin(acc[nb]);  // the products stay in this stage
+      slot = slot == R - 1 ? 0 : slot + 1;
+      if ((s & 3) == 3) {
+        pin(sn);  // a branch: as a selection it would wait for the load in every stage
+        sa = sn;
+      } else {
+        sa = (int)((uint32_t)sa >> 8);
+      }
+    };
+    int s = 0;
+    for (; s < nk - (R - 1); ++s) step(s);
+    aim(nxt, next, more);
+    const int next_row = token(next.row) * 4;
+    const int sa0 = __builtin_amdgcn_raw_buffer_load_b32(rs, next_row, 0, 0);
+    for (; s < nk; ++s) step(s);
+
+    // acc[nb][4 g + q]: row lrow, weight row 32 nb + 8 g + 4 khalf + q of the column
+    const size_t row = cur.row0 + lrow;
+    const bool mine = lrow < cur.rows;
+    if constexpr (MODE == MODE_GATEUP) {
+      float a = 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float h = swiglu(acc[0][v] * m[0], acc[1][v] * m[1]);
+        acc[0][v] = h;
+        a = fmaxf(a, finite_magnitude(h));
+      }
+      a = fmaxf(a, __shfl_xor(a, 32, 64));
+      // through the slot read last: nothing is loaded into it before the next step
+      const int free_slot = (slot == 0 ? R - 1 : slot - 1) * Cfg::SLOT;
+      asm volatile("" ::: "memory");
+      if (khalf == 0) reinterpret_cast<float*>(ring + free_slot)[lrow] = a;
+      bar_lds();
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) a = fmaxf(a, reinterpret_cast<const float*>(smem + w * kStreamLds + free_slot)[lrow]);
+      bar_lds();
+      const int e8 = scale_exponent(a);
+      const float inv = inverse_scale(e8);
+      if (mine) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<uint32_t*>(p.h + row * p.g.F + cur.col * 128 + wave * 32 + 8 * g + 4 * khalf) = pack_e4m3x4(
+              acc[0][4 * g] * inv, acc[0][4 * g + 1] * inv, acc[0][4 * g + 2] * inv, acc[0][4 * g + 3] * inv);
+        if (wave == 0 && khalf == 0) p.sh[((size_t)(cur.col >> 2) * p.g.P + row) * 4 + (cur.col & 3)] = (uint8_t)e8;
+      }
+    } else if (mine) {
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const floatx16& c = acc[nb];
+          uint2 v;
+          v.x = pack_bf16x2(c[4 * g] * m[0], c[4 * g + 1] * m[0]);
+          v.y = pack_bf16x2(c[4 * g + 2] * m[0], c[4 * g + 3] * m[0]);
+          *reinterpret_cast<uint2*>(o + row * p.g.H + cur.col * 64 + nb * 32 + 8 * g + 4 * khalf) = v;
+        }
+    }
+    if (!more) break;
+    cur = nxt;
+    sa = sa0;
+    s_row = next_row;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      word[i][0] = next.word[i][0];
+      word[i][1] = next.word[i][1];
+    }
+  }
+  wait_vm<0>();  // no load may write LDS after the wavefront has ended
+}
+
+// Whether a launch's groups are so small that it only streams weights: at most
+// 32 tokens at any layer by the bound the host has (one block of MFMA rows).
+bool stream_launch(const Fp8Problem& p) {
+  auto fits = [](int K) { return K / BKB >= kStreamMinStages && K / BKB <= kStreamMaxStages; };
+  return p.g.layer_tokens <= 32 && fits(p.g.H) && fits(p.g.F);
+}
+
+template <int MODE, int NA>
+void launch_stream_na(const Fp8Problem& p, const WeightTable& wt, bf16_t* o, hipStream_t s) {
+  // a CU's LDS holds the rings of four wavefronts
+  hipLaunchKernelGGL((stream_gemm_fp8<MODE, NA>), dim3(MODE == MODE_GATEUP ? persistent_grid() : 4 * persistent_grid()),
+                     dim3(MODE == MODE_GATEUP ? 256 : 64), 0, s, p, wt, o);
+}
+template <int MODE>
+void launch_stream(const Fp8Problem& p, const WeightTable& wt, bf16_t* o, hipStream_t s) {
+  if (p.g.layer_tokens <= 8) launch_stream_na<MODE, 1>(p, wt, o, s);
+  else if (p.g.layer_tokens <= 16) launch_stream_na<MODE, 2>(p, wt, o, s);
+  else launch_stream_na<MODE, 4>(p, wt, o, s);
+}
+
 }  // namespace
 
 hipError_t launch_gateup_fp8(const Fp8Problem& p, const WeightTable& wt, hipStream_t s) {
   prof_start(EB_K_GATEUP, s);
-  hipLaunchKernelGGL(grouped_gemm_fp8<MODE_GATEUP>, dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
+  if (stream_launch(p)) launch_stream<MODE_GATEUP>(p, wt, nullptr, s);
+  else hipLaunchKernelGGL(grouped_gemm_fp8<MODE_GATEUP>, dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
                      static_cast<bf16_t*>(nullptr), p.g.F / 128);
   prof_stop(EB_K_GATEUP, s);
   return hipGetLastError();
@@ -641,7 +956,8 @@ hipError_t launch_gateup_fp8(const Fp8Problem& p, const WeightTable& wt, hipStre
 
 hipError_t launch_down_fp8(const Fp8Problem& p, const WeightTable& wt, void* o, hipStream_t s) {
   prof_start(EB_K_DOWN, s);
-  hipLaunchKernelGGL(grouped_gemm_fp8<MODE_DOWN>, dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
+  if (stream_launch(p)) launch_stream<MODE_DOWN>(p, wt, static_cast<bf16_t*>(o), s);
+  else hipLaunchKernelGGL(grouped_gemm_fp8<MODE_DOWN>, dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
                      static_cast<bf16_t*>(o), p.g.H / BN);
   prof_stop(EB_K_DOWN, s);
   return hipGetLastError();

@@ -184,6 +184,13 @@ SIZES = [  # H, F, E, k, S, L, plan [(layer, T)]
     (8448, 128, 2, 1, 0, 1, [(0, 9)]),                # 66 K blocks: two sets of scales
     (256, 8320, 2, 1, 0, 1, [(0, 140)]),              # 65 K blocks down
     (1024, 512, 40, 6, 2, 3, [(2, 50), (0, 1), (1, 129)]),
+    # at most 32 tokens a layer and K from 8 blocks on: the streaming launches
+    (1024, 1024, 5, 2, 1, 1, [(0, 1)]),
+    (1280, 1152, 6, 2, 0, 2, [(0, 8), (1, 3)]),
+    (1024, 1408, 4, 2, 1, 1, [(0, 9), (0, 6)]),
+    (2048, 1024, 3, 1, 0, 2, [(1, 32), (0, 17)]),
+    (8448, 1024, 2, 1, 0, 1, [(0, 20)]),
+    (1024, 8320, 2, 1, 0, 1, [(0, 7)]),
 ]
 
 
@@ -244,15 +251,15 @@ def test_views_and_out_of_range_ids():
         assert torch.equal(got.view(torch.int16), c.o[:c.P].view(torch.int16))
 
 
-@pytest.mark.parametrize("T", [4, 60, 300])
-def test_a_token_that_picks_an_expert_twice(T):
+@pytest.mark.parametrize("T,H,F", [(4, 256, 128), (60, 256, 128), (300, 256, 128), (7, 1024, 1024), (32, 1024, 1024)])
+def test_a_token_that_picks_an_expert_twice(T, H, F):
     """Both slots have the same grouped row and the same result; the group's
     other rows are not read as tokens."""
     E, k = 6, 3
     rng = np.random.default_rng(T)
     picks = np.stack([rng.permutation(E)[:k] for _ in range(T)])
     picks[1::3, 2] = picks[1::3, 0]
-    c = Case(256, 128, E, k, 0, 1, [(0, T)], seed=9, idx=[picks]).run()
+    c = Case(H, F, E, k, 0, 1, [(0, T)], seed=9, idx=[picks]).run()
     torch.cuda.synchronize()
     inv = c.inv[:c.P].cpu().numpy().reshape(T, k)
     assert np.array_equal(inv[1::3, 2], inv[1::3, 0])
@@ -262,13 +269,15 @@ def test_a_token_that_picks_an_expert_twice(T):
             c.check_rows(slice(inv[t, r], inv[t, r] + 1), a[t:t + 1], 0, picks[t, r], o, hq, hs)
 
 
-def test_rows_do_not_depend_on_the_step():
-    """A micro-batch alone, and with others around it: the same bits."""
-    big = Case(512, 384, 5, 2, 1, 2, [(0, 300), (1, 45), (0, 130)], seed=10).run()
+@pytest.mark.parametrize("H,F", [(512, 384), (1024, 1152)])
+def test_rows_do_not_depend_on_the_step(H, F):
+    """A micro-batch alone, some of its tokens, and with others around it (every
+    tile shape and the streaming launches): the same bits."""
+    big = Case(H, F, 5, 2, 1, 2, [(0, 300), (1, 45), (0, 130)], seed=10).run()
     torch.cuda.synchronize()
     slots, at = 3, [0, 300, 345]
     for i, (l, T) in enumerate(big.plan):
-        for rows in ([T], [T // 3]):
+        for rows in ([T], [T // 3], [31], [16], [5], [1]):
             n = rows[0]
             one = Case.__new__(Case)
             one.__dict__.update(big.__dict__)

@@ -220,7 +220,7 @@ StepWs carve_step(const eb_model_desc& d, const StepShape& sh, const eb_step_vie
   if (d.dtype == EB_DTYPE_FP8) {
     if (b.perm == nullptr) b.perm = reinterpret_cast<int32_t*>(base + L.perm);
     b.a_perm = nullptr;
-    w.partial = nullptr;
+    w.partial = L.partial ? reinterpret_cast<float*>(base + L.partial) : nullptr;
     w.qa = base + L.qa;
     w.sa = base + L.sa;
     w.h = (views && views->h) ? views->h : base + L.h;
@@ -255,7 +255,9 @@ int run_gemms(const eb_model_desc& d, const StepShape& sh, const StepWs& w, cons
     Fp8Problem q{gp, (int32_t)sh.tokens, d.k + d.S, w.b.perm, w.qa, w.sa, static_cast<uint8_t*>(w.h), w.sh};
     if ((rc = hip_status(launch_gateup_fp8(q, wt, s), "gate/up GEMM"))) return rc;
     q.g.work_ctr = w.b.work_ctr + kWorkDown;
-    return hip_status(launch_down_fp8(q, wt, o, s), "down GEMM");
+    q.g.ksplit = down_ksplit(d.dtype, d.F);
+    q.g.partial = w.partial;
+    return hip_status(launch_down_fp8(q, wt, o, s, sum_halves), "down GEMM");
   }
   if ((rc = hip_status(launch_gateup(d.dtype, gp, wt, w.b.a_perm, w.h, s), "gate/up GEMM"))) return rc;
   gp.work_ctr = w.b.work_ctr + kWorkDown;

@@ -76,7 +76,7 @@ constexpr int kLogitsOnly = -1;
 
 // K split of the down GEMM: two halves for long K (a rule on the shape only,
 // so every schedule computes a row the same way).
-inline int down_ksplit(int dtype, int F) { return dtype == EB_DTYPE_BF16 && F >= 8192 ? 2 : 1; }
+inline int down_ksplit(int dtype, int F) { return dtype != EB_DTYPE_F32 && F >= 8192 ? 2 : 1; }
 
 // The same for an 8-bit stack: the tokens' quantised activations, read through
 // the grouping, and the quantised h.  Scales are exponents (E8M0), one byte per
@@ -258,15 +258,19 @@ hipError_t launch_gateup(int dtype, const GroupedProblem& p, const WeightTable& 
 hipError_t launch_down(int dtype, const GroupedProblem& p, const WeightTable& wt,
                        const void* h, void* o, hipStream_t s, bool sum_halves = true);
 
-// 8-bit stacks: h from qa, o (bf16) from h (gemm_fp8.hip), and what quantises
+// 8-bit stacks: h from qa, o (bf16) from h (gemm_fp8.hip; sum_halves as for
+// launch_down), and what quantises
 // (quant8.hip): a step's tokens (sa's rows: `tokens`), n matrices N x K.
 hipError_t launch_gateup_fp8(const Fp8Problem& p, const WeightTable& wt, hipStream_t s);
-hipError_t launch_down_fp8(const Fp8Problem& p, const WeightTable& wt, void* o, hipStream_t s);
+hipError_t launch_down_fp8(const Fp8Problem& p, const WeightTable& wt, void* o, hipStream_t s, bool sum_halves = true);
 hipError_t launch_quantize_rows(const RunTable& rt, int tokens, uint8_t* qa, uint32_t* sa, hipStream_t s);
 hipError_t launch_quantize_rows_dev(const RunTable* rt, int H, int tokens, uint8_t* qa, uint32_t* sa, hipStream_t s);
 hipError_t launch_copy_scales(const float* src, void* dst, size_t bytes, hipStream_t s);
 hipError_t launch_quantize_blocks(int src_dtype, int n, int N, int K, const void* src, void* q, float* scales,
                                   hipStream_t s);
+
+// o = bf16(p0 + p1) over the live rows of a split-K down GEMM's two fp32 halves.
+void launch_split_sum(const float* part, long long elems, const int32_t* P_live, int H, void* o, hipStream_t s);
 
 hipError_t launch_combine(const RunTable& rt, int dtype, const void* o, const int32_t* inv,
                           hipStream_t s);

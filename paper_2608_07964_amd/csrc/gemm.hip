@@ -1088,6 +1088,11 @@ static void launch_stream(const GroupedProblem& p, const WeightTable& wt, const 
   else launch_stream_na<MODE, 4>(p, wt, A, C, s);
 }
 
+void launch_split_sum(const float* part, long long elems, const int32_t* P_live, int H, void* o, hipStream_t s) {
+  hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)((elems / 4 + 255) / 256)), dim3(256), 0, s, part, elems, P_live,
+                     H, static_cast<bf16_t*>(o));
+}
+
 hipError_t launch_gateup(int dtype, const GroupedProblem& p, const WeightTable& wt,
                          const void* a_perm, void* h, hipStream_t s) {
   prof_start(EB_K_GATEUP, s);
@@ -1114,11 +1119,7 @@ hipError_t launch_down(int dtype, const GroupedProblem& p, const WeightTable& wt
     else
       hipLaunchKernelGGL(grouped_gemm_bf16<MODE_DOWN>, dim3(persistent_grid()), dim3(kThreads), 0, s,
                          p, wt, static_cast<const bf16_t*>(h), static_cast<bf16_t*>(o), p.H / BN);
-    if (p.ksplit > 1 && sum_halves) {
-      const long long n = (long long)p.P * p.H;
-      hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, s,
-                         p.partial, n, p.P_live, p.H, static_cast<bf16_t*>(o));
-    }
+    if (p.ksplit > 1 && sum_halves) launch_split_sum(p.partial, (long long)p.P * p.H, p.P_live, p.H, o, s);
   } else {
     hipLaunchKernelGGL(grouped_gemm_f32<MODE_DOWN>, dim3(kF32PerCu * persistent_grid()), dim3(64 * kF32Waves), 0, s,
                        p, wt, static_cast<const float*>(h), static_cast<float*>(o), p.H / FBN);

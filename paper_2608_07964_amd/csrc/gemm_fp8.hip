@@ -48,13 +48,20 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+// Weights that one workgroup alone reads, in launches that do little but stream
+// them, are loaded with the nt cache policy (see gemm.hip): the bound of the
+// tokens at one layer for which a launch counts as such.
+constexpr int kNonTemporal = 2;  // bit nt of a buffer load's cache policy
+constexpr int kNtTokens = 128;
+
 // Tiles as in gemm.hip, in bytes: a stage is 128 bytes of K of every row.
 constexpr int BN = 256, BKB = 128;
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kBLoads = BN / (8 * kWaves);       // 8-row B loads per wave per stage
 
-template <int BM_, int WM_, int SA_, int SB_>
+template <int BM_, int WM_, int SA_, int SB_, bool NT_ = false>
 struct TileCfg {
+  static constexpr int B_POLICY = NT_ ? kNonTemporal : 0;  // cache policy of the weight loads
   static constexpr int BM = BM_;
   static constexpr int WM = WM_, WN = kWaves / WM_;
   static constexpr int SA = SA_, SB = SB_;
@@ -70,6 +77,7 @@ struct TileCfg {
 using CfgBig = TileCfg<256, 2, 2, 3>;
 using CfgMid = TileCfg<128, 2, 3, 3>;
 using CfgSkinny = TileCfg<64, 2, 4, 4>;
+using CfgSkinnyNt = TileCfg<64, 2, 4, 4, true>;
 constexpr int cmax(int a, int b) { return a > b ? a : b; }
 constexpr int kLds = cmax(cmax(CfgBig::LDS, CfgMid::LDS), CfgSkinny::LDS);
 static_assert(kLds <= 160 * 1024, "LDS budget");
@@ -87,6 +95,7 @@ struct KLoop {
   int a_lane[4];                   // per-lane A byte offset of load j (row and swizzled chunk)
   int s_lane[4];                   // per-lane byte offset of the scales of fragment row block mb
   int s_stride;                    // bytes from one four-block group of scales to the next
+  int s_first;                     // byte offset of the item's first group
   int b_lane, b_tile, b_stage;     // as in gemm.hip
   int lds_a_load, lds_b_load, lds_a, lds_b;
   int sw, nk, khalf;
@@ -98,7 +107,6 @@ struct Frags {
   intx8 a[C::MB], b[C::NB];
 };
 
-constexpr int kNonTemporal = 2;  // bit nt of a buffer load's cache policy
 template <int POLICY = 0>
 __device__ __forceinline__ void load16_lds(__amdgpu_buffer_rsrc_t r, uint8_t* lds, int voff, int soff) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 16, voff, soff, 0, POLICY);
@@ -109,7 +117,7 @@ __device__ __forceinline__ void load_a(const KLoop& L, int s, int slot, int j) {
 }
 template <class C>
 __device__ __forceinline__ void load_b(const KLoop& L, int s, int slot, int j) {
-  load16_lds(L.rb, L.smem + C::B_RING + slot * C::B_BYTES + L.lds_b_load + j * 8 * BKB, L.b_lane,
+  load16_lds<C::B_POLICY>(L.rb, L.smem + C::B_RING + slot * C::B_BYTES + L.lds_b_load + j * 8 * BKB, L.b_lane,
              L.b_tile + s * L.b_stage + j * 1024);
 }
 
@@ -323,7 +331,7 @@ __device__ __forceinline__ void stage(const KLoop& L, LoopState<C>& st, floatx16
   if (BYTE == 0) {
 #pragma unroll
     for (int mb = 0; mb < NACT; ++mb)
-      sn[mb] = __builtin_amdgcn_raw_buffer_load_b32(L.rs, L.s_lane[mb], ((kt >> 2) + 1) * L.s_stride, 0);
+      sn[mb] = __builtin_amdgcn_raw_buffer_load_b32(L.rs, L.s_lane[mb], L.s_first + ((kt >> 2) + 1) * L.s_stride, 0);
   }
   st.pb_s = min(kt + C::SB, last);
   st.pb_slot = st.cb;
@@ -494,12 +502,44 @@ __device__ __forceinline__ void epilogue_down(const Fp8Problem& p, const floatx1
   }
 }
 
-template <class C, int MODE>
+// The fp32 sums of a K half: a lane's four consecutive columns at a time.
+template <class C>
+__device__ __forceinline__ void epilogue_part(const Fp8Problem& p, const floatx16 (&acc)[C::MB][C::NB], float m,
+                                              float* part, int row0, int row_end, int ni, int r0w, int wn, int nact,
+                                              int lane) {
+#pragma unroll
+  for (int mb = 0; mb < C::MB; ++mb) {
+    const int row = row0 + r0w + mb * 32 + (lane & 31);
+    if (mb >= nact || row >= row_end) continue;
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx16& c = acc[mb][nb];
+        *reinterpret_cast<float4*>(part + (size_t)row * p.g.H + ni * BN + wn * C::TN + nb * 32 + 8 * g + 4 * (lane >> 5)) =
+            make_float4(c[4 * g] * m, c[4 * g + 1] * m, c[4 * g + 2] * m, c[4 * g + 3] * m);
+      }
+  }
+}
+
+// K blocks of an item: all of them, or one of the halves that separate items
+// compute (the first a whole number of exponent words long).
+struct KPart {
+  int first, n;
+};
+__device__ __forceinline__ KPart k_part(int nk, int ksplit, int kh) {
+  if (ksplit == 1) return KPart{0, nk};
+  const int cut = (nk / 2) & ~3;
+  return kh == 0 ? KPart{0, cut} : KPart{cut, nk - cut};
+}
+
+template <class C, int MODE, bool PART>
 __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf16_t* o, const uint8_t* Bbase,
-                                         const float* scales, int row0, int row_end, int ni, int wave, int lane) {
+                                         const float* scales, int row0, int row_end, int ni, KPart kp, float* part,
+                                         int wave, int lane) {
   const int K = MODE == MODE_GATEUP ? p.g.H : p.g.F;
   const int n_rows = MODE == MODE_GATEUP ? 2 * p.g.F : p.g.H;
-  const int nk = K / BKB;
+  const int nk_all = K / BKB, nk = kp.n;
   const int wm = wave / C::WN, wn = wave % C::WN;
   const int lrow = lane & 31;
   // rows per wavefront row: the tile's rows split evenly in whole 32-row blocks
@@ -515,7 +555,7 @@ __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf1
     if constexpr (MODE == MODE_GATEUP) return min(max(p.perm[row] / p.slots, 0), p.tokens - 1);  // grouped positions that no pair maps to hold anything
     else return row;
   };
-  const int pieces = (nk + 3) / 4;
+  const int pieces = (nk_all + 3) / 4;
   if constexpr (MODE == MODE_GATEUP) {
     kl.ra = buffer_rsrc(p.qa, (uint32_t)p.tokens * (uint32_t)K);
     kl.rs = buffer_rsrc(p.sa, (uint32_t)(pieces * 4) * (uint32_t)p.tokens);
@@ -525,18 +565,19 @@ __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf1
     kl.rs = buffer_rsrc(p.sh, (uint32_t)(pieces * 4) * (uint32_t)p.g.P);
     kl.s_stride = p.g.P * 4;
   }
+  kl.s_first = (kp.first / 4) * kl.s_stride;
   const int ca = lp ^ ((((C::BM / kWaves) * wave + lr) >> 1) & 7);  // swizzle of the wave's first load row; odd j flip bit 2
 #pragma unroll
   for (int j = 0; j < C::A_LOADS; ++j) {
     const int r = (C::BM / kWaves) * wave + 8 * j + lr;
     const int at = MODE == MODE_GATEUP ? a_row(r) : r;
-    kl.a_lane[j] = row0 + r < row_end ? at * K + ((j & 1) ? ca ^ 4 : ca) * 16 : (int)0x80000000;
+    kl.a_lane[j] = row0 + r < row_end ? at * K + kp.first * BKB + ((j & 1) ? ca ^ 4 : ca) * 16 : (int)0x80000000;
   }
 #pragma unroll
   for (int mb = 0; mb < C::MB; ++mb) kl.s_lane[mb] = a_row(wm * tm + mb * 32 + lrow) * 4;
   kl.b_lane = lane * 16;
   kl.b_stage = (n_rows / BN) * (BN * BKB);
-  kl.b_tile = ni * (BN * BKB) + wave * (BN / kWaves) * BKB;
+  kl.b_tile = kp.first * kl.b_stage + ni * (BN * BKB) + wave * (BN / kWaves) * BKB;
   kl.lds_a_load = (C::BM / kWaves) * wave * BKB;
   kl.lds_b_load = (BN / kWaves) * wave * BKB;
   kl.lds_a = (wm * tm + lrow) * BKB;
@@ -547,8 +588,8 @@ __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf1
   // gate/up: column tile ni is f block ni, whose up rows' block is F/128 later;
   // down: two 128-row blocks to a column tile, two wavefront columns to a block
   constexpr int NS = MODE == MODE_GATEUP ? 2 : 1;
-  kl.wscale[0] = scales + (size_t)(MODE == MODE_GATEUP ? ni : 2 * ni + (wn >> 1)) * nk;
-  kl.wscale[1] = MODE == MODE_GATEUP ? kl.wscale[0] + (size_t)(p.g.F / 128) * nk : kl.wscale[0];
+  kl.wscale[0] = scales + (size_t)(MODE == MODE_GATEUP ? ni : 2 * ni + (wn >> 1)) * nk_all + kp.first;
+  kl.wscale[1] = MODE == MODE_GATEUP ? kl.wscale[0] + (size_t)(p.g.F / 128) * nk_all : kl.wscale[0];
 
   // the scales' first words, before the ring's loads: a wait for those covers them
   float word[NS];
@@ -556,7 +597,7 @@ __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf1
 #pragma unroll
   for (int n = 0; n < NS; ++n) word[n] = scale_word(kl.wscale[n], 0, nk, lane);
 #pragma unroll
-  for (int mb = 0; mb < C::MB; ++mb) sa[mb] = __builtin_amdgcn_raw_buffer_load_b32(kl.rs, kl.s_lane[mb], 0, 0);
+  for (int mb = 0; mb < C::MB; ++mb) sa[mb] = __builtin_amdgcn_raw_buffer_load_b32(kl.rs, kl.s_lane[mb], kl.s_first, 0);
   prologue<C>(kl);
   floatx16 acc[C::MB][C::NB];
 #pragma unroll
@@ -586,12 +627,15 @@ __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf1
   bar_lds();  // every wave is done with the ring before it is written again
   if constexpr (MODE == MODE_GATEUP)
     epilogue_gateup<C>(p, acc, m, smem, row0, row_end, ni, wave, wm, wn, tm, nact, lane);
+  else if constexpr (PART)
+    epilogue_part<C>(p, acc, m[0], part, row0, row_end, ni, wm * tm, wn, nact, lane);
   else
     epilogue_down<C>(p, acc, m[0], smem, o, row0, row_end, ni, wm * tm, wave, wn, nact, lane);
 }
 
 // Persistent grouped GEMM over the items of the step (see grouped_gemm_bf16).
-template <int MODE>
+// PART: items are K halves and leave fp32 sums.
+template <int MODE, bool PART>
 __global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, WeightTable wt, bf16_t* __restrict__ o,
                                                                 int n_ntiles) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kLds];
@@ -602,7 +646,9 @@ __global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, We
   asm volatile("" ::"v"(smem) : "memory");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  ItemQueue q(p.g, n_ntiles);  // used by thread 0 only
+  constexpr int ksplit = PART ? 2 : 1;
+  const int nsub = n_ntiles * ksplit;  // items per m-tile
+  ItemQueue q(p.g, nsub);  // used by thread 0 only
   const int ES = p.g.E + p.g.S;
   const size_t mat = (size_t)(MODE == MODE_GATEUP ? 2 : 1) * p.g.F * p.g.H;  // bytes of an expert's matrix
 
@@ -614,9 +660,14 @@ __global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, We
   while (it >= 0) {
     int got = 0;
     if (tid == 0) got = q.draw();
-    const int4 gd = scalar_record(p.g.tiles, it / n_ntiles);  // key, first row, rows, first m-tile
+    const int4 gd = scalar_record(p.g.tiles, it / nsub);  // key, first row, rows, first m-tile
     const int mt = (gd.z + BM - 1) / BM;
-    const Tile2 tile = item_tile(it - gd.w * n_ntiles, mt, n_ntiles);
+    // within the group: K part slowest (see grouped_gemm_bf16)
+    const int local = it - gd.w * nsub;
+    const int kh = PART ? local / (mt * n_ntiles) : 0;
+    const Tile2 tile = item_tile(local - kh * mt * n_ntiles, mt, n_ntiles);
+    const KPart kp = k_part((MODE == MODE_GATEUP ? p.g.H : p.g.F) / BKB, ksplit, kh);
+    float* part = PART ? p.g.partial + (size_t)kh * p.g.P * p.g.H : nullptr;
     // the group's mt m-tiles share its rows evenly (whole 32-row blocks)
     const int rpt = 32 * ((gd.z + 32 * mt - 1) / (32 * mt));
     const int row0 = gd.y + tile.mi * rpt, row_end = min(gd.y + gd.z, row0 + rpt);
@@ -626,11 +677,13 @@ __global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, We
     const float* scales = reinterpret_cast<const float*>(W + ES * mat) + e * (mat / (128 * 128));
     const int rows = row_end - row0;
     if (rows > CfgMid::BM)
-      run_item<CfgBig, MODE>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, wave, lane);
+      run_item<CfgBig, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave, lane);
     else if (rows > CfgSkinny::BM)
-      run_item<CfgMid, MODE>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, wave, lane);
+      run_item<CfgMid, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave, lane);
+    else if (p.g.layer_tokens <= kNtTokens)
+      run_item<CfgSkinnyNt, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave, lane);
     else
-      run_item<CfgSkinny, MODE>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, wave, lane);
+      run_item<CfgSkinny, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave, lane);
     if (tid == 0) *s_next = q.settle(got);
     bar_lds();
     it = __builtin_amdgcn_readfirstlane(*s_next);
@@ -664,6 +717,7 @@ constexpr int kStreamMaxStages = 128; // two scale words a lane
 struct StreamUnit {
   int row0, rows, row_end;         // the chunk's first row, its rows, the end of the m-tile's rows
   int col;                         // column tile (gate/up) or 64-row column (down)
+  int kh;                          // K half of a split
   const uint8_t* B;
   const float* scales;             // of the expert's matrix
 };
@@ -681,21 +735,24 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
   uint8_t* ring = smem + wave * kStreamLds;
   const int K = MODE == MODE_GATEUP ? p.g.H : p.g.F;
   const int n_rows = MODE == MODE_GATEUP ? 2 * p.g.F : p.g.H;
-  const int nk = K / BKB, pieces = (nk + 3) / 4;
-  const int n_cols = n_rows / (64 * WAVES);          // units of an m-tile
+  const int nk_all = K / BKB, pieces = (nk_all + 3) / 4;
+  const int ksplit = MODE == MODE_DOWN ? p.g.ksplit : 1;
+  const int n_cols = n_rows / (64 * WAVES), nsub = n_cols * ksplit;  // units of an m-tile
   const int ES = p.g.E + p.g.S;
   const size_t mat = (size_t)n_rows * K;
   const int b_stage = (n_rows / BN) * (BN * BKB);    // bytes from one K stage's blocks to the next one's
 
-  const long long total = (long long)(*p.g.n_tiles) * n_cols;
+  const long long total = (long long)(*p.g.n_tiles) * nsub;
   const int xcd = blockIdx.x % kXcds, per_xcd = gridDim.x / kXcds;
   const int u_end = (int)(((xcd + 1) * total) / kXcds);
   auto decode = [&](int unit) {
     StreamUnit d;
     const int u = __builtin_amdgcn_readfirstlane(unit);
-    const int4 gd = scalar_record(p.g.tiles, u / n_cols);  // key, first row, rows, first m-tile
+    const int4 gd = scalar_record(p.g.tiles, u / nsub);  // key, first row, rows, first m-tile
     const int mt = (gd.z + BM - 1) / BM;
-    const int local = u - gd.w * n_cols;             // column, m-tile fastest
+    int local = u - gd.w * nsub;                     // K part, then column, m-tile fastest
+    d.kh = local / (mt * n_cols);
+    local -= d.kh * mt * n_cols;
     d.col = local / mt;
     const int rpt = 32 * ((gd.z + 32 * mt - 1) / (32 * mt));
     d.row0 = gd.y + (local - d.col * mt) * rpt;
@@ -723,11 +780,12 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
     }
     const int r = d.row0 + min(lrow, d.rows - 1);
     n.row = MODE == MODE_GATEUP ? p.perm[r] : r;
-    const float* s = d.scales + (size_t)(MODE == MODE_GATEUP ? d.col : d.col / 2) * nk;
+    const KPart kp = k_part(nk_all, ksplit, d.kh);
+    const float* s = d.scales + (size_t)(MODE == MODE_GATEUP ? d.col : d.col / 2) * nk_all + kp.first;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      n.word[i][0] = scale_word(s + (size_t)i * (p.g.F / 128) * nk, 0, nk, lane);
-      n.word[i][1] = scale_word(s + (size_t)i * (p.g.F / 128) * nk, 64, nk, lane);
+      n.word[i][0] = scale_word(s + (size_t)i * (p.g.F / 128) * nk_all, 0, kp.n, lane);
+      n.word[i][1] = scale_word(s + (size_t)i * (p.g.F / 128) * nk_all, 64, kp.n, lane);
     }
   };
   // token of a pair (gate/up); grouped positions that no pair maps to hold anything
@@ -742,14 +800,15 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
   int a_voff[NA], a_soff = 0, b_voff = 0;
   auto aim = [&](const StreamUnit& d, const Ahead& n, bool any) {  // any false: no next unit, loads of empty buffers
     const int base = MODE == MODE_GATEUP ? 0 : d.row0;
+    const KPart kp = k_part(nk_all, ksplit, d.kh);
     ra = buffer_rsrc(uniform((MODE == MODE_GATEUP ? p.qa : p.h) + (size_t)base * K),
                      __builtin_amdgcn_readfirstlane(any ? (MODE == MODE_GATEUP ? p.tokens : d.rows) * K : 0));
-    rb = buffer_rsrc(uniform(d.B + (MODE == MODE_GATEUP ? (size_t)d.col * (BN * BKB) + wave * (64 * BKB)
+    rb = buffer_rsrc(uniform(d.B + (size_t)kp.first * b_stage + (MODE == MODE_GATEUP ? (size_t)d.col * (BN * BKB) + wave * (64 * BKB)
                                                        : (size_t)(d.col >> 2) * (BN * BKB) + (d.col & 3) * (64 * BKB))),
-                     __builtin_amdgcn_readfirstlane(any ? (nk - 1) * b_stage + 64 * BKB : 0));
+                     __builtin_amdgcn_readfirstlane(any ? (kp.n - 1) * b_stage + 64 * BKB : 0));
 #pragma unroll
     for (int j = 0; j < NA; ++j)
-      a_voff[j] = 8 * j + lr < d.rows ? (token(n.a[j]) - base) * K + ((j & 1) ? c_even ^ 4 : c_even) * 16 : (int)0x80000000;
+      a_voff[j] = 8 * j + lr < d.rows ? (token(n.a[j]) - base) * K + kp.first * BKB + ((j & 1) ? c_even ^ 4 : c_even) * 16 : (int)0x80000000;
     a_soff = 0;
     b_voff = lane * 16;
   };
@@ -773,7 +832,11 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
   // scales of the unit being multiplied: weight words, the rows' exponents of
   // four K blocks (sa) and of the next four (sn)
   float word[NS][2];
-  int s_row = token(next.row) * 4;
+  // (byte offset of a row's first exponent word)
+  auto s_at = [&](const StreamUnit& d, const Ahead& n) {
+    return token(n.row) * 4 + (k_part(nk_all, ksplit, d.kh).first / 4) * s_stride;
+  };
+  int s_row = s_at(cur, next);
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
     word[i][0] = next.word[i][0];
@@ -801,6 +864,7 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
       if (more) nxt = decode(u);
     }
     ahead(nxt, next);
+    const int nk = k_part(nk_all, ksplit, cur.kh).n;
     WeightScales ws[NS][2];
     float m[2] = {1.f, 1.f};
     bool scaled = false;
@@ -865,7 +929,7 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
     int s = 0;
     for (; s < nk - (R - 1); ++s) step(s);
     aim(nxt, next, more);
-    const int next_row = token(next.row) * 4;
+    const int next_row = s_at(nxt, next);
     const int sa0 = __builtin_amdgcn_raw_buffer_load_b32(rs, next_row, 0, 0);
     for (; s < nk; ++s) step(s);
 
@@ -904,6 +968,12 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const floatx16& c = acc[nb];
+          if (ksplit > 1) {
+            *reinterpret_cast<float4*>(p.g.partial + ((size_t)cur.kh * p.g.P + row) * p.g.H + cur.col * 64 + nb * 32 +
+                                       8 * g + 4 * khalf) =
+                make_float4(c[4 * g] * m[0], c[4 * g + 1] * m[0], c[4 * g + 2] * m[0], c[4 * g + 3] * m[0]);
+            continue;
+          }
           uint2 v;
           v.x = pack_bf16x2(c[4 * g] * m[0], c[4 * g + 1] * m[0]);
           v.y = pack_bf16x2(c[4 * g + 2] * m[0], c[4 * g + 3] * m[0]);
@@ -926,8 +996,9 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
 // Whether a launch's groups are so small that it only streams weights: at most
 // 32 tokens at any layer by the bound the host has (one block of MFMA rows).
 bool stream_launch(const Fp8Problem& p) {
-  auto fits = [](int K) { return K / BKB >= kStreamMinStages && K / BKB <= kStreamMaxStages; };
-  return p.g.layer_tokens <= 32 && fits(p.g.H) && fits(p.g.F);
+  // (halves of at least 32 blocks, where K is split)
+  auto fits = [](int nk) { return nk >= kStreamMinStages && nk <= kStreamMaxStages; };
+  return p.g.layer_tokens <= 32 && fits(p.g.H / BKB) && fits(p.g.F / BKB);
 }
 
 template <int MODE, int NA>
@@ -948,17 +1019,22 @@ void launch_stream(const Fp8Problem& p, const WeightTable& wt, bf16_t* o, hipStr
 hipError_t launch_gateup_fp8(const Fp8Problem& p, const WeightTable& wt, hipStream_t s) {
   prof_start(EB_K_GATEUP, s);
   if (stream_launch(p)) launch_stream<MODE_GATEUP>(p, wt, nullptr, s);
-  else hipLaunchKernelGGL(grouped_gemm_fp8<MODE_GATEUP>, dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
+  else hipLaunchKernelGGL((grouped_gemm_fp8<MODE_GATEUP, false>), dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
                      static_cast<bf16_t*>(nullptr), p.g.F / 128);
   prof_stop(EB_K_GATEUP, s);
   return hipGetLastError();
 }
 
-hipError_t launch_down_fp8(const Fp8Problem& p, const WeightTable& wt, void* o, hipStream_t s) {
+hipError_t launch_down_fp8(const Fp8Problem& p, const WeightTable& wt, void* o, hipStream_t s, bool sum_halves) {
   prof_start(EB_K_DOWN, s);
   if (stream_launch(p)) launch_stream<MODE_DOWN>(p, wt, static_cast<bf16_t*>(o), s);
-  else hipLaunchKernelGGL(grouped_gemm_fp8<MODE_DOWN>, dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
-                     static_cast<bf16_t*>(o), p.g.H / BN);
+  else if (p.g.ksplit > 1)
+    hipLaunchKernelGGL((grouped_gemm_fp8<MODE_DOWN, true>), dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
+                       static_cast<bf16_t*>(o), p.g.H / BN);
+  else
+    hipLaunchKernelGGL((grouped_gemm_fp8<MODE_DOWN, false>), dim3(persistent_grid()), dim3(kThreads), 0, s, p, wt,
+                       static_cast<bf16_t*>(o), p.g.H / BN);
+  if (p.g.ksplit > 1 && sum_halves) launch_split_sum(p.g.partial, (long long)p.g.P * p.g.H, p.g.P_live, p.g.H, o, s);
   prof_stop(EB_K_DOWN, s);
   return hipGetLastError();
 }

@@ -54,6 +54,46 @@ def pack_expert_weights(desc, W_gu, W_dn) -> None:
             _packed[id(t)] = t
 
 
+def pack_expert_weights_fp8(desc, W_gu, W_dn) -> tuple:
+    """8-bit expert weights of an EB_DTYPE_FP8 stack, one packed buffer a layer
+    and kind (easybalance_pack_weights_fp8): returns the lists for W_gu and W_dn.
+    A layer is either its matrices in bf16 or fp32, row-major ([E+S][2F][H] and
+    [E+S][H][F]), which are quantised (easybalance_quantize_weights), or a
+    checkpoint's pair (e4m3 values of that shape, fp32 scales by 128 x 128 block).
+    What comes in is left as it is."""
+    out = []
+    for layers, kind in ((W_gu, B.EB_WEIGHTS_GATE_UP), (W_dn, B.EB_WEIGHTS_DOWN)):
+        packed = []
+        N, K = (2 * desc.F, desc.H) if kind == B.EB_WEIGHTS_GATE_UP else (desc.H, desc.F)
+        n = desc.E + desc.S
+        for w in layers:
+            parts = w if isinstance(w, (tuple, list)) else (w,)
+            if not all(t.is_cuda and t.is_contiguous() for t in parts):
+                raise ValueError("expert weights must be contiguous device tensors")
+            if tuple(parts[0].shape) != (n, N, K):
+                raise ValueError(f"expert weights must have shape {(n, N, K)}, not {tuple(parts[0].shape)}")
+            dev = parts[0].device
+            stream = torch.cuda.current_stream(dev)
+            if len(parts) == 1:
+                if w.dtype not in (torch.bfloat16, torch.float32):
+                    raise ValueError(f"expert weights to quantise must be bf16 or fp32, not {w.dtype}")
+                q = torch.empty(n, N, K, dtype=torch.float8_e4m3fn, device=dev)
+                scales = torch.empty(n, N // 128, K // 128, dtype=torch.float32, device=dev)
+                B.easybalance_quantize_weights(desc, kind, n, w, q, scales, stream.cuda_stream)
+            else:
+                q, scales = parts
+                if q.dtype not in (torch.float8_e4m3fn, torch.uint8) or scales.dtype != torch.float32 or \
+                        tuple(scales.shape) != (n, N // 128, K // 128):
+                    raise ValueError("8-bit weights are (e4m3 values, fp32 scales by 128 x 128 block)")
+            dst = torch.empty(B.easybalance_packed_fp8_size(desc, kind, n), dtype=torch.uint8, device=dev)
+            B.easybalance_pack_weights_fp8(desc, kind, n, q, scales, dst, stream.cuda_stream)
+            del q, scales  # freed in stream order, after the pack
+            _packed[id(dst)] = dst
+            packed.append(dst)
+        out.append(packed)
+    return tuple(out)
+
+
 @dataclasses.dataclass
 class StepRecord:
     runset: list            # [(j, l_j)] in ascending j
@@ -68,17 +108,24 @@ class Stack:
     x [N][T][H] fp32 is updated in place.  Inputs: gain [L][H] fp32,
     Wg [L] -> [E][H], bias [L][E] fp32, W_gu [L] -> [E+S][2F][H],
     W_dn [L] -> [E+S][H][F] (dtype of the stack), the expert weights packed
-    by pack_expert_weights.
+    by pack_expert_weights.  dtype "fp8": Wg in bf16, W_gu and W_dn from
+    pack_expert_weights_fp8.  router: a binding.make_router struct, the choice
+    of experts in place of the softmax top-k; balance [L][E] fp32 or None: its
+    bias.
     """
 
     def __init__(self, *, L, H, F, E, k, S, D, N, T, dtype, x, gain, Wg, bias, W_gu, W_dn,
-                 eps=1e-6, norm_topk=0, device="cuda:0"):
+                 eps=1e-6, norm_topk=0, device="cuda:0", router=None, balance=None):
         self.L, self.H, self.F, self.E, self.k, self.S, self.D, self.N, self.T = \
             L, H, F, E, k, S, D, N, T
         self.dtype = dtype
         self.desc = B.make_desc(L, H, F, E, k, S, D, dtype, eps, norm_topk)
         self.dev = torch.device(device)
-        tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        tdt = torch.bfloat16 if dtype in ("bf16", "fp8") else torch.float32
+        self.router, self.balance = router, balance
+        if balance is not None and (router is None or balance.shape != (L, E) or balance.dtype != torch.float32
+                                    or not balance.is_contiguous()):
+            raise ValueError("balance is a contiguous fp32 [L][E] tensor and goes with a router")
         self.x, self.gain, self.Wg, self.bias, self.W_gu, self.W_dn = x, gain, Wg, bias, W_gu, W_dn
         assert x.shape == (N, T, H) and x.dtype == torch.float32 and x.is_contiguous()
         if not all(is_packed(t) for t in list(W_gu) + list(W_dn)):
@@ -99,6 +146,12 @@ class Stack:
 
     # ---- the three operations of Algorithm 1 -------------------------------
     def route(self, j: int, layer: int, stream) -> None:
+        if self.router is not None:
+            B.easybalance_route_scored(self.desc, self.router, layer, self.T, self.x[j], self.gain[layer],
+                                       self.Wg[layer], self.bias[layer],
+                                       None if self.balance is None else self.balance[layer], self.a[j],
+                                       self.logits[j], self.idx[j], self.w[j], self.counts[j], stream)
+            return
         B.easybalance_route(self.desc, layer, self.T, self.x[j], self.gain[layer], self.Wg[layer],
                             self.bias[layer], self.a[j], self.logits[j], self.idx[j], self.w[j],
                             self.counts[j], stream)
@@ -132,10 +185,14 @@ class Stack:
             self._state_bytes = B.easybalance_pass_state_size(self.desc, self.N, self.T)
             self._state = torch.empty(self._state_bytes + 256, dtype=torch.uint8, device=self.dev)
         sp = self._state.data_ptr() + (-self._state.data_ptr()) % 256
-        n, rs, ly, sl, gr, ll = B.easybalance_run_pass(
-            self.desc, self.N, self.T, self.x, self.gain, self.Wg, self.bias, self.W_gu, self.W_dn,
-            pol, m, sp, self._state_bytes, max_steps=self.N * self.L, record=record,
-            stream=stream.cuda_stream, placement=placement)
+        tail = (self.W_gu, self.W_dn, pol, m, sp, self._state_bytes)
+        kw = dict(max_steps=self.N * self.L, record=record, stream=stream.cuda_stream, placement=placement)
+        if self.router is not None:
+            n, rs, ly, sl, gr, ll = B.easybalance_run_pass_scored(
+                self.desc, self.router, self.N, self.T, self.x, self.gain, self.Wg, self.bias, self.balance, *tail, **kw)
+        else:
+            n, rs, ly, sl, gr, ll = B.easybalance_run_pass(
+                self.desc, self.N, self.T, self.x, self.gain, self.Wg, self.bias, *tail, **kw)
         if not record:
             return []
         self.layer_loads = ll.astype(np.int64)

@@ -89,7 +89,8 @@ extern "C" {
  * where the router counts too (the choice under an eb_router is always
  * ROUTE_TOPK); the grouping of a small step runs as one
  * kernel, reported as PERM_SCAN (with the gather's copies in the smallest); an
- * 8-bit step gathers no rows, PERM_GATHER is the quantisation of its tokens. */
+ * 8-bit step gathers no rows, PERM_GATHER is the quantisation of its tokens (part
+ * of PERM_SCAN in small steps). */
 #define EB_K_ROUTE_NORM 0
 #define EB_K_ROUTE_LOGITS 1
 #define EB_K_ROUTE_TOPK 2

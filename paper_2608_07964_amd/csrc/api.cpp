@@ -217,12 +217,17 @@ StepWs carve_step(const eb_model_desc& d, const StepShape& sh, const eb_step_vie
   b.perm = views ? views->perm : nullptr;
   b.inv = inv;
   w.qa = w.sa = w.sh = nullptr;
+  b.qa = nullptr;
+  b.sa = nullptr;
+  b.q_tokens = 0;
   if (d.dtype == EB_DTYPE_FP8) {
     if (b.perm == nullptr) b.perm = reinterpret_cast<int32_t*>(base + L.perm);
     b.a_perm = nullptr;
     w.partial = L.partial ? reinterpret_cast<float*>(base + L.partial) : nullptr;
-    w.qa = base + L.qa;
+    b.qa = w.qa = base + L.qa;
     w.sa = base + L.sa;
+    b.sa = reinterpret_cast<uint32_t*>(w.sa);
+    b.q_tokens = (int32_t)sh.tokens;
     w.h = (views && views->h) ? views->h : base + L.h;
     w.sh = static_cast<uint8_t*>(w.h) + (size_t)sh.P * d.F;
     return w;
@@ -252,7 +257,13 @@ int run_gemms(const eb_model_desc& d, const StepShape& sh, const StepWs& w, cons
   gp.partial = nullptr;
   int rc;
   if (d.dtype == EB_DTYPE_FP8) {
-    Fp8Problem q{gp, (int32_t)sh.tokens, d.k + d.S, w.b.perm, w.qa, w.sa, static_cast<uint8_t*>(w.h), w.sh};
+    // division by k + S = n as a product, exact below 2^31: with 2^s the power of
+    // two from n on, m = ceil(2^(31 + s) / n) is less than 2^32 and off by less than 1
+    uint32_t s2 = 0, mul = 0;
+    const uint32_t n = (uint32_t)(d.k + d.S);
+    while ((1u << s2) < n) ++s2;
+    if (n > 1) mul = (uint32_t)(((1ull << (31 + s2)) + n - 1) / n);
+    Fp8Problem q{gp, (int32_t)sh.tokens, mul, n > 1 ? s2 - 1 : 0, w.b.perm, w.qa, w.sa, static_cast<uint8_t*>(w.h), w.sh};
     if ((rc = hip_status(launch_gateup_fp8(q, wt, s), "gate/up GEMM"))) return rc;
     q.g.work_ctr = w.b.work_ctr + kWorkDown;
     q.g.ksplit = down_ksplit(d.dtype, d.F);
@@ -328,10 +339,6 @@ int enqueue_step_dev(const eb_model_desc& d, int N, int T, const RunTable* rt, c
   const StepWs w = carve_step(d, sh, nullptr, ws, inv);
   int rc;
   if ((rc = hip_status(launch_permute_dev(d, rt, N, T, w.b, s), "permute")))
-    return rc;
-  if (d.dtype == EB_DTYPE_FP8 &&
-      (rc = hip_status(launch_quantize_rows_dev(rt, d.H, (int)sh.tokens, w.qa, reinterpret_cast<uint32_t*>(w.sa), s),
-                       "quantisation")))
     return rc;
   // a split-K down GEMM leaves its two fp32 halves for the combine, which
   // rounds their sum as the split-K sum kernel would (o is not stored)
@@ -535,10 +542,6 @@ int moe_step_common(const eb_model_desc* desc, int32_t n_run, const eb_work* run
 
   const RunTable rt = make_run_table(d, n_run, run, nullptr);
   if ((rc = hip_status(launch_permute(d, rt, w.b, s), "permute"))) return rc;
-  if (d.dtype == EB_DTYPE_FP8 &&
-      (rc = hip_status(launch_quantize_rows(rt, (int)sh.tokens, w.qa, reinterpret_cast<uint32_t*>(w.sa), s),
-                       "quantisation")))
-    return rc;
   return run_gemms(d, sh, w, wt, o_out, s);
 }
 

@@ -84,7 +84,8 @@ inline int down_ksplit(int dtype, int F) { return dtype != EB_DTYPE_F32 && F >= 
 // ((block / 4) * rows + row) * 4 + block % 4.
 struct Fp8Problem {
   GroupedProblem g;
-  int32_t tokens, slots;                   // tokens the buffers hold; k + S
+  int32_t tokens;                          // tokens the buffers hold
+  uint32_t div_mul, div_shift;             // pair / (k + S) = umulhi(pair, div_mul) >> div_shift (div_mul 0: pair)
   const int32_t* perm;                     // [P] pair at each grouped position
   const uint8_t* qa;                       // [tokens][H]
   const uint8_t* sa;                       // [ceil(H / 512)][tokens][4]
@@ -231,7 +232,10 @@ struct StepBuffers {
   int32_t max_tiles;
   int32_t* perm;           // or null: only an 8-bit step reads it, else it is for callers that ask
   int32_t* inv;
-  void* a_perm;            // or null (8-bit steps): no rows are gathered
+  void* a_perm;            // or null (8-bit steps): no rows are gathered, but the tokens
+  uint8_t* qa;             // quantised: values [tokens][H] and exponents (Fp8Problem),
+  uint32_t* sa;            // sa's rows: q_tokens
+  int32_t q_tokens;
 };
 
 // Grouping of a step: perm, inv, offsets, tile list, a_perm; work counters
@@ -263,8 +267,8 @@ hipError_t launch_down(int dtype, const GroupedProblem& p, const WeightTable& wt
 // (quant8.hip): a step's tokens (sa's rows: `tokens`), n matrices N x K.
 hipError_t launch_gateup_fp8(const Fp8Problem& p, const WeightTable& wt, hipStream_t s);
 hipError_t launch_down_fp8(const Fp8Problem& p, const WeightTable& wt, void* o, hipStream_t s, bool sum_halves = true);
-hipError_t launch_quantize_rows(const RunTable& rt, int tokens, uint8_t* qa, uint32_t* sa, hipStream_t s);
-hipError_t launch_quantize_rows_dev(const RunTable* rt, int H, int tokens, uint8_t* qa, uint32_t* sa, hipStream_t s);
+template <class RTA>
+hipError_t launch_quantize_rows(RTA rt, int H, int grid_tokens, int tokens, uint8_t* qa, uint32_t* sa, hipStream_t s);
 hipError_t launch_copy_scales(const float* src, void* dst, size_t bytes, hipStream_t s);
 hipError_t launch_quantize_blocks(int src_dtype, int n, int N, int K, const void* src, void* q, float* scales,
                                   hipStream_t s);

@@ -86,6 +86,13 @@ constexpr int BM = CfgBig::BM;
 // largest values per wavefront column, and the next item's index.
 constexpr int kTileLds = BM * 128, kMaxLds = kTileLds, kNextLds = kMaxLds + 4 * BM * 4;
 
+// Token of a pair (gate/up reads its rows through the grouping; positions that
+// no pair maps to hold anything).
+__device__ __forceinline__ int token_of_pair(const Fp8Problem& p, int pair) {
+  const uint32_t q = (uint32_t)pair, t = p.div_mul ? __umulhi(q, p.div_mul) >> p.div_shift : q;
+  return (int)min(t, (uint32_t)(p.tokens - 1));
+}
+
 // An item's loads.  A rows come from anywhere (gate/up: the token of the
 // grouped position), so every A load has its own lane offset; a row past the
 // item's end has one past the buffer's end, which reads zeros.
@@ -411,6 +418,27 @@ __device__ __forceinline__ void k_loop_nact(const KLoop& kl, floatx16 (&acc)[C::
   }
 }
 
+// acc0 = h = SiLU(m0 acc0) * (m1 acc1); returns the largest finite |h|.  The
+// maximum passes over NaN by itself; infinities (which become NaN, so that
+// they are quantised as such) are looked for only where one is the maximum.
+__device__ __forceinline__ float swiglu16(floatx16& acc0, const floatx16& acc1, const float (&m)[2]) {
+  float a = 0.f;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    acc0[v] = swiglu(acc0[v] * m[0], acc1[v] * m[1]);
+    a = fmaxf(a, fabsf(acc0[v]));
+  }
+  if (__any(a == INFINITY)) {
+    a = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      acc0[v] = nan_if_infinite(acc0[v]);
+      a = fmaxf(a, fabsf(acc0[v]));
+    }
+  }
+  return a;
+}
+
 // Gate/up epilogue: the item's 128 columns of h are one scale block of the
 // down GEMM.  A lane holds 16 of a row's columns; their largest |h| meets
 // those of the other lanes and wavefront columns through LDS, then the row is
@@ -424,13 +452,7 @@ __device__ __forceinline__ void epilogue_gateup(const Fp8Problem& p, floatx16 (&
 #pragma unroll
   for (int mb = 0; mb < C::MB; ++mb) {
     if (mb >= nact) continue;
-    float a = 0.f;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const float h = swiglu(acc[mb][0][v] * m[0], acc[mb][1][v] * m[1]);
-      acc[mb][0][v] = h;
-      a = fmaxf(a, finite_magnitude(h));
-    }
+    float a = swiglu16(acc[mb][0], acc[mb][1], m);
     a = fmaxf(a, __shfl_xor(a, 32, 64));
     if (khalf == 0) mx[wn * BM + wm * tm + mb * 32 + lrow] = a;
   }
@@ -552,7 +574,7 @@ __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf1
   // row of the A buffer and of the scales that tile row r is
   auto a_row = [&](int r) {
     const int row = min(row0 + r, row_end - 1);
-    if constexpr (MODE == MODE_GATEUP) return min(max(p.perm[row] / p.slots, 0), p.tokens - 1);  // grouped positions that no pair maps to hold anything
+    if constexpr (MODE == MODE_GATEUP) return token_of_pair(p, p.perm[row]);
     else return row;
   };
   const int pieces = (nk_all + 3) / 4;
@@ -788,8 +810,8 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
       n.word[i][1] = scale_word(s + (size_t)i * (p.g.F / 128) * nk_all, 64, kp.n, lane);
     }
   };
-  // token of a pair (gate/up); grouped positions that no pair maps to hold anything
-  auto token = [&](int v) { return MODE == MODE_GATEUP ? min(max(v / p.slots, 0), p.tokens - 1) : v; };
+  // row of the A buffer that a loaded value stands for
+  auto token = [&](int v) { return MODE == MODE_GATEUP ? token_of_pair(p, v) : v; };
 
   // load cursor
   const __amdgpu_buffer_rsrc_t rs = MODE == MODE_GATEUP
@@ -937,13 +959,7 @@ __global__ __launch_bounds__(MODE == MODE_GATEUP ? 256 : 64, 1) void stream_gemm
     const size_t row = cur.row0 + lrow;
     const bool mine = lrow < cur.rows;
     if constexpr (MODE == MODE_GATEUP) {
-      float a = 0.f;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const float h = swiglu(acc[0][v] * m[0], acc[1][v] * m[1]);
-        acc[0][v] = h;
-        a = fmaxf(a, finite_magnitude(h));
-      }
+      float a = swiglu16(acc[0], acc[1], m);
       a = fmaxf(a, __shfl_xor(a, 32, 64));
       // through the slot read last: nothing is loaded into it before the next step
       const int free_slot = (slot == 0 ? R - 1 : slot - 1) * Cfg::SLOT;

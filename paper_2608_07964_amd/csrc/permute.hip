@@ -24,6 +24,7 @@
 // All results are integers fixed by the inputs (no order-dependent atomics).
 #include "eb_internal.h"
 #include "eb_numeric.h"
+#include "quant_rows.h"
 
 namespace eb {
 namespace {
@@ -307,7 +308,14 @@ template <class RTA>
 __global__ __launch_bounds__(kScanThreads) void perm_small_kernel(
     RTA rta, int32_t* __restrict__ offsets, int4* __restrict__ tiles, int bm, TailRule tail, int max_tiles,
     int32_t* __restrict__ work_ctr, int32_t* __restrict__ perm, int32_t* __restrict__ inv, int row_bytes,
-    uint8_t* __restrict__ a_perm) {
+    uint8_t* __restrict__ a_perm, uint8_t* __restrict__ qa, uint32_t* __restrict__ sa, int q_tokens) {
+  // 8-bit steps: the workgroups after the first quantise the tokens, which the
+  // grouping has nothing to do with (a launch less)
+  if (blockIdx.x > 0) {
+    quantize_row_piece(rta.get(), (long long)(blockIdx.x - 1) * kScanWaves + (threadIdx.x >> 6),
+                       (rta.get().H + 511) / 512, q_tokens, qa, sa);
+    return;
+  }
   __shared__ int running[kMaxKeys];                        // per-key totals, then offsets / cursors
   __shared__ unsigned long long masks[kSmallWords / 2];    // [pieces][E] lanes per expert, then the counts
   __shared__ int wtot[kScanWaves], s_layer[kSmallPieces];
@@ -530,10 +538,11 @@ bool perm_small(const eb_model_desc& d, int pieces, int chunks) {
 }
 
 template <class RTA>
-void perm_small_impl(RTA a, const StepBuffers& b, int bm, TailRule tail, int row_bytes, hipStream_t s) {
+void perm_small_impl(RTA a, const StepBuffers& b, int bm, TailRule tail, int row_bytes, int q_waves, hipStream_t s) {
   prof_start(EB_K_PERM_SCAN, s);
-  hipLaunchKernelGGL(perm_small_kernel<RTA>, dim3(1), dim3(kScanThreads), 0, s, a, b.offsets, b.tiles, bm, tail,
-                     b.max_tiles, b.work_ctr, b.perm, b.inv, row_bytes, static_cast<uint8_t*>(b.a_perm));
+  hipLaunchKernelGGL(perm_small_kernel<RTA>, dim3(1 + (q_waves + kScanWaves - 1) / kScanWaves), dim3(kScanThreads),
+                     0, s, a, b.offsets, b.tiles, bm, tail, b.max_tiles, b.work_ctr, b.perm, b.inv, row_bytes,
+                     static_cast<uint8_t*>(b.a_perm), b.qa, b.sa, b.q_tokens);
   prof_stop(EB_K_PERM_SCAN, s);
 }
 
@@ -562,14 +571,15 @@ void permute_impl(RTA a, const eb_model_desc& d, int grid_chunks, int grid_token
   const bool gather = b.a_perm != nullptr;
   if (perm_small(d, pieces, grid_chunks)) {
     const bool copy = gather && (long long)grid_tokens * (d.k + d.S) * d.H * elem_bytes <= kSmallCopy;
-    perm_small_impl(a, b, bm, tail, copy ? d.H * elem_bytes : 0, s);
-    if (copy) return;
+    perm_small_impl(a, b, bm, tail, copy ? d.H * elem_bytes : 0, gather ? 0 : grid_tokens * ((d.H + 511) / 512), s);
+    if (copy || !gather) return;
   } else {
     perm_count_impl(a, grid_chunks, b.hist, s);
     perm_scan_impl(a, b.hist, b.chunk_base, b.offsets, b.tiles, bm, tail, b.max_tiles, b.work_ctr, s);
     perm_scatter_impl(a, grid_chunks, b.chunk_base, b.perm, b.inv, s);
   }
-  if (gather) gather_impl(a, d.H, grid_tokens, elem_bytes, b.inv, b.a_perm, s);
+  if (!gather) (void)launch_quantize_rows(a, d.H, grid_tokens, b.q_tokens, b.qa, b.sa, s);  // status: hipGetLastError
+  else gather_impl(a, d.H, grid_tokens, elem_bytes, b.inv, b.a_perm, s);
 }
 
 bool scan_fits(int L, int E, int S, int n) {

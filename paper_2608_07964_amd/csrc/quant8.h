@@ -13,11 +13,6 @@
 
 namespace eb {
 
-__device__ __forceinline__ float finite_magnitude(float v) {
-  const float a = fabsf(v);
-  return a < INFINITY ? a : 0.f;  // NaN fails the comparison too
-}
-
 // Biased exponent (x + 127) of the scale of a block whose largest finite
 // magnitude is amax = 1.f 2^y: y - 8 where 1.f <= 1.75, else y - 7.
 __device__ __forceinline__ int scale_exponent(float amax) {
@@ -31,13 +26,13 @@ __device__ __forceinline__ float scale_value(int e8) {
   return e8 == 0 ? 0x1p-127f : __uint_as_float((uint32_t)e8 << 23);
 }
 
-// Four values of magnitude at most 448 (or not finite) to e4m3, the first in
-// the low byte.  An infinity is turned into a NaN first: what the conversion
-// makes of it depends on a mode bit.
+// Four values of magnitude at most 448, or NaN, to e4m3, the first in the low
+// byte.  Infinities are to be NaN before: what the conversion makes of them
+// depends on a mode bit.
 __device__ __forceinline__ float nan_if_infinite(float v) { return fabsf(v) == INFINITY ? __builtin_nanf("") : v; }
 __device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(nan_if_infinite(a), nan_if_infinite(b), 0, false);
-  r = __builtin_amdgcn_cvt_pk_fp8_f32(nan_if_infinite(c), nan_if_infinite(d), r, true);
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
   return (uint32_t)r;
 }
 

@@ -166,6 +166,15 @@ __device__ __forceinline__ void pin(T& v) {
   asm volatile("" : "+v"(v));
 }
 
+// The lane's number, made anew: what is computed from it is computed where it
+// is used, not once ahead of all items and kept in scratch memory (a load from
+// there waits for the whole ring).
+__device__ __forceinline__ int fresh_lane() {
+  int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+  pin(lane);
+  return lane;
+}
+
 // Half h (64 bytes of K) of a fragment row: 16-byte chunks 4 h + khalf and
 // 4 h + 2 + khalf, the same for both operands, so the products pair up.
 template <class C>
@@ -558,7 +567,8 @@ __device__ __forceinline__ KPart k_part(int nk, int ksplit, int kh) {
 template <class C, int MODE, bool PART>
 __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf16_t* o, const uint8_t* Bbase,
                                          const float* scales, int row0, int row_end, int ni, KPart kp, float* part,
-                                         int wave, int lane) {
+                                         int wave) {
+  const int lane = fresh_lane();
   const int K = MODE == MODE_GATEUP ? p.g.H : p.g.F;
   const int n_rows = MODE == MODE_GATEUP ? 2 * p.g.F : p.g.H;
   const int nk_all = K / BKB, nk = kp.n;
@@ -648,11 +658,11 @@ __device__ __forceinline__ void run_item(const Fp8Problem& p, uint8_t* smem, bf1
   else k_loop_nact<C, false, NS>(kl, acc, sa, ws, nact, lane);
   bar_lds();  // every wave is done with the ring before it is written again
   if constexpr (MODE == MODE_GATEUP)
-    epilogue_gateup<C>(p, acc, m, smem, row0, row_end, ni, wave, wm, wn, tm, nact, lane);
+    epilogue_gateup<C>(p, acc, m, smem, row0, row_end, ni, wave, wm, wn, tm, nact, fresh_lane());
   else if constexpr (PART)
-    epilogue_part<C>(p, acc, m[0], part, row0, row_end, ni, wm * tm, wn, nact, lane);
+    epilogue_part<C>(p, acc, m[0], part, row0, row_end, ni, wm * tm, wn, nact, fresh_lane());
   else
-    epilogue_down<C>(p, acc, m[0], smem, o, row0, row_end, ni, wm * tm, wave, wn, nact, lane);
+    epilogue_down<C>(p, acc, m[0], smem, o, row0, row_end, ni, wm * tm, wave, wn, nact, fresh_lane());
 }
 
 // Persistent grouped GEMM over the items of the step (see grouped_gemm_bf16).
@@ -666,7 +676,7 @@ __global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, We
   int* s_next = reinterpret_cast<int*>(smem + (MODE == MODE_GATEUP ? kNextLds : 0));
   // the LDS ring is written by global->LDS loads the compiler does not see
   asm volatile("" ::"v"(smem) : "memory");
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   constexpr int ksplit = PART ? 2 : 1;
   const int nsub = n_ntiles * ksplit;  // items per m-tile
@@ -699,13 +709,13 @@ __global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, We
     const float* scales = reinterpret_cast<const float*>(W + ES * mat) + e * (mat / (128 * 128));
     const int rows = row_end - row0;
     if (rows > CfgMid::BM)
-      run_item<CfgBig, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave, lane);
+      run_item<CfgBig, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave);
     else if (rows > CfgSkinny::BM)
-      run_item<CfgMid, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave, lane);
+      run_item<CfgMid, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave);
     else if (p.g.layer_tokens <= kNtTokens)
-      run_item<CfgSkinnyNt, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave, lane);
+      run_item<CfgSkinnyNt, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave);
     else
-      run_item<CfgSkinny, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave, lane);
+      run_item<CfgSkinny, MODE, PART>(p, smem, o, Bbase, scales, row0, row_end, tile.ni, kp, part, wave);
     if (tid == 0) *s_next = q.settle(got);
     bar_lds();
     it = __builtin_amdgcn_readfirstlane(*s_next);

@@ -280,14 +280,20 @@ __device__ __forceinline__ bool choose_fp32(const eb_router& p, const TeamMap& m
       x = fmaxf(x, o1);
     }
     const float gs = p.group_top == 2 ? x + y : x;
-    int before = 0;
-    for (int g = 0; g < p.n_group; ++g) before += __shfl(gs, g * m.lpg, W) > gs;
+    int before = 0, upto = 0;
+    for (int g = 0; g < p.n_group; ++g) {
+      const float o = __shfl(gs, g * m.lpg, W);
+      before += o > gs;
+      upto += o >= gs;
+    }
     const bool real = m.group < p.n_group, kept = real && before < p.topk_group;
     // the last group kept against the first left out, each at its worst
     const float size = fabsf(x) + (p.group_top == 2 ? fabsf(y) : 0.f), err = floor + 2 * kMarginSum * size;
     const float in = team_reduce<W>(kept ? err + Key::ERROR * size - gs : ninf, maxf);
     const float out = team_reduce<W>(real && !kept ? gs + err : ninf, maxf);
     near |= !(-in > out) || (real && !(gs - gs == 0.f));
+    // groups equal here (their keys have fewer digits than their scores) across the bound
+    near |= kept && upto > p.topk_group;
 #pragma unroll
     for (int i = 0; i < DEPTH; ++i) key[i] = kept ? key[i] : 0u;
   }

@@ -92,6 +92,26 @@ def test_ties_go_to_the_lower_id(score):
     check(np.where(z > 0, -0.0, 0.0), 6, **kw)
 
 
+@pytest.mark.parametrize("T", [40, 300, 5300])
+@pytest.mark.parametrize("E,G", [(256, 8), (64, 4), (480, 10)])
+def test_close_groups_are_decided_exactly(E, G, T):
+    """Groups whose scores differ by less than the fp32 choice tells apart,
+    while the picks among them are far from one another."""
+    rng = np.random.default_rng(E + T)
+    step = 2.0 ** rng.integers(-23, -16, size=(T, 1))
+    total = 1.3 + step * np.argsort(rng.random((T, G)), axis=1)
+    c = 0.3 * rng.random((T, G, E // G))
+    c[:, :, 3] = 0.66 + 0.2 * rng.random((T, G))
+    c[:, :, 11] = total - c[:, :, 3]
+    z = np.log(c / (1 - c)).reshape(T, E).astype(np.float32)
+    kw = dict(score="sigmoid", n_group=G, topk_group=G // 2)
+    if T <= 300:
+        return check(z, 4, **kw)
+    idx, w, _ = run_select(z, 4, **kw)
+    rows = rng.choice(T, 300, replace=False)
+    assert np.array_equal(idx[rows], o8.select(z[rows], 4, **kw)[0])
+
+
 @pytest.mark.parametrize("score", ["sigmoid", "softmax"])
 def test_close_scores_are_decided_exactly(score):
     """Scores a few fp32 steps apart, told apart by the logits or the balance only."""

@@ -500,36 +500,49 @@ int lane_experts(const eb_router& p, int E, int W) {
 // 53.3 / 22.0; of 64 experts: 1024 7.8 / 12.9, 4096 11.5 / 13.1, 6144 14.7 / 12.2.
 constexpr int kWholeWaveBlocks = 160;
 // Most tokens of an entry for which one workgroup takes all of them and writes
-// the counts itself: one a wavefront (32 tokens, two a wavefront, took 11.3 us,
-// 33 with the counts cleared by a launch before 8.7).
-constexpr int kOwnTokens = 16;
+// the counts itself, which saves the launch that clears them: 16 by one whole
+// wavefront each, more by quarters (1024 threads where a lane has up to 8
+// experts, else 512, whose registers hold 16).  In us, so / with the launch
+// before: 60 experts, 17 tokens 6.2 / 10.8, 64 7.0 / 10.9, 128 9.2 / 11.0, 192
+// 11.1 / 11.0; 128 experts, 32 tokens 6.8 / 11.6, 128 11.4 / 12.0; 256 experts in
+// 8 groups, 32 tokens 8.5 / 12.8, 64 12.2 / 12.8, 96 15.8 / 13.0.
+constexpr int kOwnWaves = 16, kOwnQuarters8 = 128, kOwnQuarters16 = 64;
+int own_tokens(const eb_router& p, int E, int k) {
+  const int v16 = lane_experts(p, E, 16);
+  if (v16 > 0 && v16 <= 8) return kOwnQuarters8;
+  return v16 > 0 && v16 <= 16 && k <= 8 ? kOwnQuarters16 : kOwnWaves;
+}
 
-// OWN: every entry has 1 to kOwnTokens tokens.  A token takes a whole wavefront where that
-// leaves none waiting; above, a quarter of one, which costs fewer instructions.
+// OWN: every entry has 1 to own_tokens() tokens, at most `most`.  A token takes
+// a whole wavefront where that leaves none waiting; above, a quarter of one,
+// which costs fewer instructions.
 template <bool OWN, class RBA>
-void select_dispatch(RBA rba, const eb_router& p, int E, int k, int entries, int blocks, hipStream_t s) {
+void select_dispatch(RBA rba, const eb_router& p, int E, int k, int entries, int blocks, int most, hipStream_t s) {
   // a lane's 16 experts in a quarter of a wavefront are at most 4 in a whole one
   const int v16 = lane_experts(p, E, 16), v64 = lane_experts(p, E, 64);
-  constexpr int SMALL = 16, LARGE = OWN ? 16 : 128, TH = OWN ? 256 : 1024, REST = OWN ? 16 : 32;
-  if (blocks <= kWholeWaveBlocks && v64 <= 1) select_launch<64, 1, 1, 1, 1024, SMALL, OWN>(rba, p, E, k, entries, blocks, s);
-  else if (blocks <= kWholeWaveBlocks && v64 <= 4) select_launch<64, 4, 4, 4, 1024, SMALL, OWN>(rba, p, E, k, entries, blocks, s);
-  else if (v16 > 0 && v16 <= 4) select_launch<16, 4, 4, 4, TH, LARGE, OWN>(rba, p, E, k, entries, blocks, s);
-  else if (v16 > 0 && v16 <= 8) select_launch<16, 8, 8, 4, TH, LARGE, OWN>(rba, p, E, k, entries, blocks, s);
-  else if (v16 > 0 && v16 <= 16 && k <= 8) select_launch<16, 16, 9, 4, TH, LARGE, OWN>(rba, p, E, k, entries, blocks, s);
-  else if (v16 > 0 && v16 <= 16) select_launch<16, 16, 16, 4, TH, LARGE, OWN>(rba, p, E, k, entries, blocks, s);
+  const bool whole = OWN ? most <= kOwnWaves : blocks <= kWholeWaveBlocks;
+  constexpr int LARGE8 = OWN ? kOwnQuarters8 : 128, LARGE16 = OWN ? kOwnQuarters16 : 128, TH16 = OWN ? 512 : 1024;
+  constexpr int REST = OWN ? kOwnWaves : 32;
+  if (whole && v64 <= 1) select_launch<64, 1, 1, 1, 1024, 16, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (whole && v64 <= 4) select_launch<64, 4, 4, 4, 1024, 16, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (v16 > 0 && v16 <= 4) select_launch<16, 4, 4, 4, 1024, LARGE8, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (v16 > 0 && v16 <= 8) select_launch<16, 8, 8, 4, 1024, LARGE8, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (v16 > 0 && v16 <= 16 && k <= 8) select_launch<16, 16, 9, 4, TH16, LARGE16, OWN>(rba, p, E, k, entries, blocks, s);
+  else if (!OWN && v16 > 0 && v16 <= 16) select_launch<16, 16, 16, 4, 1024, 128, false>(rba, p, E, k, entries, blocks, s);
   else if (v64 <= 8) select_launch<64, 8, 8, 8, 256, REST, OWN>(rba, p, E, k, entries, blocks, s);
   else select_launch<64, 32, 32, 32, 256, REST, OWN>(rba, p, E, k, entries, blocks, s);
 }
 
 template <class RBA>
-hipError_t select_batch(RBA rba, const eb_router& p, int E, int k, int grid_entries, int grid_blocks, bool own,
-                        hipStream_t s) {
+hipError_t select_batch(RBA rba, const eb_router& p, int E, int k, int grid_entries, int grid_blocks, int least,
+                        int most, hipStream_t s) {
+  const bool own = least >= 1 && most <= own_tokens(p, E, k);
   prof_start(EB_K_ROUTE_TOPK, s);
   if (!own && grid_entries > 0)
     hipLaunchKernelGGL((counts_clear_kernel<RBA>), dim3(grid_entries), dim3(256), 0, s, rba, E);
   if (grid_blocks > 0) {
-    if (own) select_dispatch<true>(rba, p, E, k, grid_entries, grid_blocks, s);
-    else select_dispatch<false>(rba, p, E, k, grid_entries, grid_blocks, s);
+    if (own) select_dispatch<true>(rba, p, E, k, grid_entries, grid_blocks, most, s);
+    else select_dispatch<false>(rba, p, E, k, grid_entries, grid_blocks, most, s);
   }
   prof_stop(EB_K_ROUTE_TOPK, s);
   return hipGetLastError();
@@ -538,18 +551,18 @@ hipError_t select_batch(RBA rba, const eb_router& p, int E, int k, int grid_entr
 }  // namespace
 
 hipError_t launch_select_batch(const eb_router& p, int E, int k, const RouteBatch& rb, hipStream_t s) {
-  bool one = true;
+  int least = 1, most = 0;
   for (int i = 0; i < rb.n; ++i) {
     const int T = rb.tok0[i + 1] - rb.tok0[i];
-    one = one && T >= 1 && T <= kOwnTokens;
+    least = T < least ? T : least;
+    most = T > most ? T : most;
   }
-  return select_batch(ByValue<RouteBatch>{rb}, p, E, k, rb.n, rb.blk0[rb.n], one, s);
+  return select_batch(ByValue<RouteBatch>{rb}, p, E, k, rb.n, rb.blk0[rb.n], least, most, s);
 }
 
 hipError_t launch_select_batch_dev(const eb_router& p, int E, int k, const RouteBatch* rb, int max_entries, int T,
                                    hipStream_t s) {
-  return select_batch(InMemory<RouteBatch>{rb}, p, E, k, max_entries, max_entries * ((T + 31) / 32),
-                      T >= 1 && T <= kOwnTokens, s);
+  return select_batch(InMemory<RouteBatch>{rb}, p, E, k, max_entries, max_entries * ((T + 31) / 32), T, T, s);
 }
 
 }  // namespace eb

@@ -80,6 +80,16 @@ def test_token_counts(T):
     assert np.array_equal(idx[rows], want[0]) and np.allclose(w[rows], want[1], rtol=W_REL, atol=0)
 
 
+@pytest.mark.parametrize("E,k", [(60, 4), (128, 16), (256, 8), (200, 12)])
+def test_where_one_workgroup_takes_an_entry(E, k):
+    """Token counts on both sides of every bound of that, by the experts of a lane."""
+    rng = np.random.default_rng(E)
+    z, bal = rng.normal(size=(129, E)).astype(np.float32), (rng.normal(size=E) * 0.05).astype(np.float32)
+    for T in (16, 17, 63, 64, 65, 127, 128, 129):
+        check(z[:T], k, balance=bal, score="sigmoid")
+        check(np.round(z[:T]), k, score="softmax")  # ties, all of them decided again
+
+
 @pytest.mark.parametrize("score", ["sigmoid", "softmax"])
 def test_ties_go_to_the_lower_id(score):
     rng = np.random.default_rng(5)

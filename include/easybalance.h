@@ -212,8 +212,8 @@ typedef struct eb_router {
 
 /*
  * easybalance_select -- experts, weights and counts of T tokens from their
- * router logits, under `router` (see eb_router).  One launch for up to 16
- * tokens, else two.
+ * router logits, under `router` (see eb_router).  One launch for up to 16 to 128
+ * tokens (by E, n_group and k), else two.
  *
  * logits     device [T][E] fp32
  * balance    device [E] fp32, or NULL

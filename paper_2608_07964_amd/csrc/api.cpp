@@ -1,7 +1,7 @@
 // C ABI of libeasybalance.so: argument checks, workspace layout, per-step
 // tables, kernel-timing hooks.  The compute lives in the kernels of
-// route.hip, permute.hip, gemm.hip and combine.hip; the scheduler in
-// schedule.cpp.
+// route.hip, select.hip, permute.hip, quant8.hip, gemm.hip, gemm_fp8.hip and
+// combine.hip; the scheduler in schedule.cpp.
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>

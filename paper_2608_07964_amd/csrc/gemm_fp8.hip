@@ -35,6 +35,20 @@
 //
 // Every output accumulates its blocks in ascending order, whatever tile or
 // group its row sits in: rows give the same bits in every schedule.
+//
+// Bounds and rates.  Launches of few rows an expert are bound by streaming the
+// weights, of many by the matrix cores (3.0 PFLOP/s in a large library product
+// with one scale for all; reads reach 6.2 TB/s):
+//   one token, 64 + 2 experts of H = 2048, F = 1408     gate/up 16 us, down 10
+//   81 tokens on three layers of 60 + 4 of them         74 (6.0 TB/s), 40 (5.6)
+//   64 tokens, 8 experts of H = 4096, F = 14336         155 (6.1 TB/s), 79 (6.0)
+//   3072 tokens on five layers of the first shape       414 (4.6 TB/s), 228 (4.2)
+//   8192 tokens, 256 + 1 experts of H = 7168, F = 2048  2150 (2.0 PFLOP/s), 1260 (1.7)
+// In the last a stage takes 2610 cycles where its matrix instructions take 2010
+// (LDS moves 256 KB a stage), an item's start and end are another 11% (gate/up)
+// and 23% (down), and the clock falls to 1.8 GHz.  Starting the next item's weight
+// loads before the epilogue hid most of the start and gained nothing (3518
+// against 3521 us a step; the stages of smaller launches took longer by as much).
 #include "eb_internal.h"
 #include "eb_numeric.h"
 #include "gemm_items.h"
@@ -50,7 +64,8 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 // Weights that one workgroup alone reads, in launches that do little but stream
 // them, are loaded with the nt cache policy (see gemm.hip): the bound of the
-// tokens at one layer for which a launch counts as such.
+// tokens at one layer for which a launch counts as such.  64 tokens on 8 experts
+// of H = 4096, F = 14336, without / with: gate/up 185 / 176 us, down 114 / 109.
 constexpr int kNonTemporal = 2;  // bit nt of a buffer load's cache policy
 constexpr int kNtTokens = 128;
 
@@ -451,7 +466,8 @@ __device__ __forceinline__ float swiglu16(floatx16& acc0, const floatx16& acc1, 
 // Gate/up epilogue: the item's 128 columns of h are one scale block of the
 // down GEMM.  A lane holds 16 of a row's columns; their largest |h| meets
 // those of the other lanes and wavefront columns through LDS, then the row is
-// quantised, collected in LDS and stored as whole 128-byte lines.
+// quantised, collected in LDS and stored as whole 128-byte lines.  Eight to nine
+// thousand cycles for 256 rows, most of them SiLU's exponential and reciprocal.
 template <class C>
 __device__ __forceinline__ void epilogue_gateup(const Fp8Problem& p, floatx16 (&acc)[C::MB][C::NB], const float (&m)[2],
                                                 uint8_t* smem, int row0, int row_end, int ni, int wave, int wm, int wn,
@@ -554,7 +570,9 @@ __device__ __forceinline__ void epilogue_part(const Fp8Problem& p, const floatx1
 }
 
 // K blocks of an item: all of them, or one of the halves that separate items
-// compute (the first a whole number of exponent words long).
+// compute (the first a whole number of exponent words long).  Whole / halves and
+// their sum, at F = 14336, H = 4096 on 8 experts (the rule is down_ksplit's): 64
+// tokens at one layer 109 / 87 + 5 us, 1425 at two 350 / 298 + 19.
 struct KPart {
   int first, n;
 };
@@ -734,7 +752,10 @@ __global__ __launch_bounds__(kThreads, 1) void grouped_gemm_fp8(Fp8Problem p, We
 // wavefront and meets nobody.  What a unit needs to find its rows and scales
 // (positions of the grouping, scale words) is loaded a unit ahead: a wait for it
 // would be a wait for the whole ring.
-// Each output is the same chain of operations as in grouped_gemm_fp8.
+// Each output is the same chain of operations as in grouped_gemm_fp8.  Against
+// its items, in us: 81 tokens on three layers of 60 + 4 experts of H = 2048, F =
+// 1408 gate/up 107 -> 75, down 60 -> 40 (weights at 6.0 and 5.6 TB/s); one token
+// on 64 + 2 24 -> 17, 18 -> 10.
 constexpr int kStreamLds = 40 * 1024;
 template <int NA>
 struct StreamCfg {

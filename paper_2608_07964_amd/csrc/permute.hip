@@ -20,6 +20,9 @@
 //                        the piece, read once, to a_perm[inv[q]] for each of
 //                        the token's k+S pairs q
 //
+// An 8-bit step gathers no rows (its GEMM reads a token's through perm); its
+// tokens are quantised instead (quant_rows.h).
+//
 // Pair q = (tok_base[rho] + t) * (k+S) + r; key = layer*(E+S) + slot expert.
 // All results are integers fixed by the inputs (no order-dependent atomics).
 #include "eb_internal.h"
@@ -310,7 +313,8 @@ __global__ __launch_bounds__(kScanThreads) void perm_small_kernel(
     int32_t* __restrict__ work_ctr, int32_t* __restrict__ perm, int32_t* __restrict__ inv, int row_bytes,
     uint8_t* __restrict__ a_perm, uint8_t* __restrict__ qa, uint32_t* __restrict__ sa, int q_tokens) {
   // 8-bit steps: the workgroups after the first quantise the tokens, which the
-  // grouping has nothing to do with (a launch less)
+  // grouping has nothing to do with (a launch less: one token's step on 64 + 2
+  // experts of H = 2048, F = 1408 37 -> 34 us)
   if (blockIdx.x > 0) {
     quantize_row_piece(rta.get(), (long long)(blockIdx.x - 1) * kScanWaves + (threadIdx.x >> 6),
                        (rta.get().H + 511) / 512, q_tokens, qa, sa);

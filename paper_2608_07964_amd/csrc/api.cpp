@@ -440,6 +440,8 @@ int easybalance_select(int32_t T, int32_t E, int32_t k, const eb_router* router,
   if (T < 0) return set_error(EB_ERR_INVALID_ARG, "T=%d < 0", T);
   const int rc = check_router(router, E, k);
   if (rc) return rc;
+  // a launch has fewer than 2^32 threads, 8 a token or 8 experts
+  if (T > 1 << 28) return set_error(EB_ERR_UNSUPPORTED, "T=%d > 2^28", T);
   if (counts_out == nullptr) return set_error(EB_ERR_INVALID_ARG, "counts_out is NULL");
   if (T > 0 && (logits == nullptr || idx_out == nullptr || w_out == nullptr))
     return set_error(EB_ERR_INVALID_ARG, "a required select pointer is NULL");

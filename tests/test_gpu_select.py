@@ -80,6 +80,22 @@ def test_token_counts(T):
     assert np.array_equal(idx[rows], want[0]) and np.allclose(w[rows], want[1], rtol=W_REL, atol=0)
 
 
+def test_logits_of_more_than_2_to_the_31_values():
+    B = _binding()
+    T, E, k = 2 ** 25 + 2 ** 19 + 77, 64, 6
+    z = torch.empty(T, E, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    idx = torch.empty(T, k, dtype=torch.int32, device="cuda")
+    w = torch.empty(T, k, device="cuda")
+    counts = torch.empty(E, dtype=torch.int32, device="cuda")
+    B.easybalance_select(T, E, k, B.make_router("sigmoid"), z, None, idx, w, counts,
+                         torch.cuda.current_stream().cuda_stream)
+    assert counts.sum().item() == T * k and int(idx.min()) >= 0 and int(idx.max()) < E
+    for at in (0, 2 ** 25 - 50, T - 100):
+        want = o8.select(z[at:at + 100].cpu().numpy(), k, score="sigmoid")
+        assert np.array_equal(idx[at:at + 100].cpu().numpy(), want[0])
+        assert np.allclose(w[at:at + 100].cpu().numpy(), want[1], rtol=W_REL, atol=0)
+
+
 @pytest.mark.parametrize("E,k", [(60, 4), (128, 16), (256, 8), (200, 12)])
 def test_where_one_workgroup_takes_an_entry(E, k):
     """Token counts on both sides of every bound of that, by the experts of a lane."""

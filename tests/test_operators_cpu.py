@@ -76,6 +76,7 @@ def test_select_refusals():
         refused(BAD, f, *select_args(router=B.make_router(**kw)))
     refused(BAD, f, *select_args(k=5, router=B.make_router(n_group=4, topk_group=1)))  # 4 experts are left
     refused(NO, f, *select_args(E=1025))
+    refused(NO, f, *select_args(T=2 ** 28 + 1))
     refused(NO, f, *select_args(E=1024, k=17))
     refused(NO, f, *select_args(E=130, router=B.make_router(n_group=65, topk_group=65)))
 

@@ -42,7 +42,7 @@
 //   one token, 64 + 2 experts of H = 2048, F = 1408     gate/up 16 us, down 10
 //   81 tokens on three layers of 60 + 4 of them         74 (6.0 TB/s), 40 (5.6)
 //   64 tokens, 8 experts of H = 4096, F = 14336         155 (6.1 TB/s), 79 (6.0)
-//   3072 tokens on five layers of the first shape       414 (4.6 TB/s), 228 (4.2)
+//   12 x 256 on five layers of the first shape          414 (4.6 TB/s), 228 (4.2)
 //   8192 tokens, 256 + 1 experts of H = 7168, F = 2048  2150 (2.0 PFLOP/s), 1260 (1.7)
 // In the last a stage takes 2610 cycles where its matrix instructions take 2010
 // (LDS moves 256 KB a stage), an item's start and end are another 11% (gate/up)
